@@ -444,6 +444,111 @@ typedef struct dc_signals_out {   /* device, [batch][max_window]; any but status
 
 DC_API int dc_signals_static(const dc_signals_in* in, const dc_signals_out* out, void* cuda_stream);
 
+/* ---- operators around a K / V cache ----------------------------------------------------------
+ * The pieces of a layer that a caller needs who drives the backbone himself: to keep contexts in 8 bits, and to
+ * run rows over a cache that see one another by a mask (a tree of drafted tokens, candidates for one block).  No
+ * paper counterpart: the paper takes the backbone and its cache as given (Section 5.1, 5.2).
+ *
+ * These calls have no context.  They enqueue work on cuda_stream (a stream of the current device, whose memory
+ * all device pointers are) and return; they allocate nothing, so they can be captured into a graph, which then
+ * holds the host lengths.  Two calls at once are independent as long as neither writes what the other reads or
+ * writes (a workspace included).  Host arrays are read during the call.  After a refusal nothing was launched
+ * and dc_last_error(NULL) gives the reason.  Strides count elements.
+ *
+ * A cache: every layer's K and V of max_batch slots in the layouts of dc_step, in the model's type (then these are
+ * the very arrays that dc_step, dc_prefill and dc_generate take) or in 8 bits.  Held in 8 bits, a row (one key of one kv
+ * head) is e4m3 values and a scale for all of them:
+ *     s = max(a / 448, 2^-80),   a = the largest finite magnitude of the row
+ *     held = e4m3(x * (1 / s)) to nearest even, infinities as +-448, NaN as NaN;   it stands for held * s
+ * (fp32, each operation rounded).  K and V of a 128-dim row take 264 bytes instead of 512. */
+enum { DC_E4M3 = 2 };    /* dc_cache.dtype, beside DC_F32 and DC_BF16 */
+
+typedef struct dc_cache {
+  int32_t dtype;          /* DC_F32 | DC_BF16 | DC_E4M3                                     */
+  int32_t n_layers, max_batch, n_kv_heads;
+  int32_t max_ctx;        /* multiple of 64                                                 */
+  int32_t head_dim;       /* multiple of 8, 8 .. 256                                        */
+  void* k;                /* device [n_layers][max_batch][n_kv_heads][max_ctx][head_dim]    */
+  void* v;                /* device [n_layers][max_batch][n_kv_heads][head_dim][max_ctx]    */
+  float *k_scale, *v_scale; /* device [n_layers][max_batch][n_kv_heads][max_ctx]; DC_E4M3 only, else null */
+} dc_cache;
+
+/* Rows of K and V outside a cache: row r of sequence b (cache slot b) is key pos[b] + r. */
+typedef struct dc_cache_rows {
+  int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
+  int32_t layer, n_layers; /* layers layer .. layer + n_layers - 1 of the cache             */
+  int32_t dtype;          /* of the rows, DC_F32 | DC_BF16; a cache that is not DC_E4M3 has the same */
+  void *k, *v;            /* device; starts of layer 0, sequence 0, row 0, kv head 0, dim 0 */
+  int64_t k_stride[5];    /* layer, sequence, row, kv head, dim: any, but 16-byte rows that */
+  int64_t v_stride[5];    /* start on 16-byte boundaries move fastest (V: dims or keys as the contiguous axis) */
+  const int32_t* pos;     /* host [batch], >= 0                                             */
+  const int32_t* n;       /* host [batch], >= 0 rows; pos[b] + n[b] <= max_ctx              */
+} dc_cache_rows;
+
+/* Writes the rows into the cache: in 8 bits with their scales, or as they are.  Every other key is left as it was. */
+DC_API int dc_cache_write(const dc_cache* cache, const dc_cache_rows* rows, void* cuda_stream);
+
+/* Reads n[b] keys from pos[b] on into the rows (a multiplication and one rounding to the rows' type); k and v are
+ * written, at different places for every value, and nothing else.  With the strides of a bf16 / fp32 cache
+ * the rows become the context of a later dc_step. */
+DC_API int dc_cache_read(const dc_cache* cache, const dc_cache_rows* rows, void* cuda_stream);
+
+/* Norm of each query and key head, and its rotation, in one pass:
+ *     y = x / sqrt(mean(x^2) + eps) * gain,   pairs (i, i + head_dim/2) turned by pos * rope_theta^(-2i/head_dim)
+ * in fp32 with the angles in fp64 (a far position keeps its fractions of a turn), rounded once.  Outputs may be the inputs
+ * themselves (same pointer, same strides); otherwise they must not overlap them. */
+typedef struct dc_qk_in {
+  int32_t dtype;          /* DC_F32 | DC_BF16: of the heads, the gains and the outputs      */
+  int32_t rows;           /* >= 0                                                           */
+  int32_t n_q_heads, n_kv_heads; /* >= 0: with 0 of either only the other is made           */
+  int32_t head_dim;       /* even, 2 .. 256; the dims of a head are contiguous              */
+  float eps;              /* >= 0                                                           */
+  float rope_theta;       /* > 0                                                            */
+  const void *q, *k;      /* device                                                         */
+  int64_t q_stride[2], k_stride[2];         /* row, head                                    */
+  const void *q_gain, *k_gain;              /* device [head_dim], or null: gains of 1       */
+  const int32_t* pos;     /* device [rows]: absolute positions                              */
+  void *q_out, *k_out;    /* device                                                         */
+  int64_t q_out_stride[2], k_out_stride[2]; /* row, head                                    */
+} dc_qk_in;
+DC_API int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream);
+
+/* Attention of drafted rows over a cache that holds their keys too: of sequence b (slot b), the keys
+ * ctx_len[b] .. ctx_len[b] + n_rows[b] - 1 are those of its rows 0 .. n_rows[b] - 1 (written by dc_cache_write).  Row r
+ * sees all ctx_len[b] keys before them, and drafted key j if bit j of its mask is set (its own key too only by its bit):
+ *     o = softmax(scale * q K^T) V    over the keys that it sees; without any, o = 0
+ * Query head h uses kv head h / (n_q_heads / n_kv_heads).  What the cache holds at other keys does not matter, NaN included;
+ * a row that sees a drafted key whose V has a value that is not finite becomes NaN in every dim, one that does not see it
+ * is not touched by it.  Sums and softmax in fp32.  On the tensor cores (bf16 rows, head_dim 128, cache of bf16 or e4m3, arrays
+ * on 16-byte boundaries) probabilities are rounded to 8 significant bits, as bf16 has. */
+typedef struct dc_tree_in {
+  int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
+  int32_t layer;          /* of the cache                                                   */
+  int32_t dtype;          /* of q and o, DC_F32 | DC_BF16; a cache that is not DC_E4M3 has the same */
+  int32_t n_q_heads;      /* a multiple of the cache's n_kv_heads                           */
+  int32_t max_rows;       /* 1 .. DC_MAX_WINDOW: row pitch of the mask                      */
+  float scale;            /* 0: 1 / sqrt(head_dim)                                          */
+  const void* q;          /* device; the dims of a head are contiguous                      */
+  void* o;                /* device; rows >= n_rows[b] are left as they were                */
+  int64_t q_stride[3], o_stride[3]; /* sequence, row, head                                  */
+  const int32_t* ctx_len; /* host [batch], >= 0; ctx_len[b] + n_rows[b] <= max_ctx          */
+  const int32_t* n_rows;  /* host [batch], 0 .. max_rows; 0: the sequence has nothing to do */
+  const uint32_t* mask;   /* device [batch][max_rows][(max_rows + 31) / 32]: bit j % 32 of word j / 32; null: all rows
+                             of a sequence see one another (a block)                        */
+  void* workspace;        /* device, 16-byte boundary; partial results, nothing is kept there between calls */
+  uint64_t workspace_bytes;
+  int32_t* status;        /* device [1] or null: set to DC_ERR_TIMEOUT where a bounded wait ran out (the rows
+                             concerned are then NaN), otherwise left as it was              */
+} dc_tree_in;
+DC_API int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, void* cuda_stream);
+
+/* The workspace that dc_tree_attention wants for these lengths (pointers to device memory are not looked at, but for their alignment). */
+DC_API int dc_tree_attention_workspace(const dc_cache* cache, const dc_tree_in* in, uint64_t* bytes);
+
+/* The mask of a tree, on the host: parent[r] < r is the row that row r continues, -1 none (it continues the context).
+ * Row r sees itself, its parent and what that one sees.  mask [n][words], words >= (n + 31) / 32. */
+DC_API int dc_tree_mask(const int32_t* parent, int32_t n, int32_t words, uint32_t* mask);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,14 +14,15 @@ _LIB_PATH = os.path.join(_HERE, "libdepcap.so")
 
 DC_OK = 0
 DC_ERR_TIMEOUT, DC_ERR_INDEX, DC_ERR_NUMERIC = 6, 7, 8
-DC_F32, DC_BF16 = 0, 1
+DC_F32, DC_BF16, DC_E4M3 = 0, 1, 2
 DC_STEP_INFLUENCE, DC_STEP_BOUNDARY, DC_STEP_EXPORT_KV, DC_STEP_CARRIED_PREV = 1, 2, 4, 8
 DC_IMPL_AUTO, DC_IMPL_SIMT = 0, 1
 STAGE_NAMES = ["embed", "norm", "qkv", "attn", "oproj", "gateup", "down", "lmhead", "xlogp",
                "boundary", "dense"]
 EXPORTS = ["dc_create", "dc_step", "dc_boundary", "dc_select", "dc_destroy", "dc_last_error",
            "dc_debug_logits", "dc_step_profiled", "dc_signals_static", "dc_commit", "dc_generate", "dc_prefill",
-           "dc_set_option", "dc_boundary_batched", "dc_select_batched"]
+           "dc_set_option", "dc_boundary_batched", "dc_select_batched", "dc_cache_write", "dc_cache_read",
+           "dc_qk_norm_rope", "dc_tree_attention", "dc_tree_attention_workspace", "dc_tree_mask"]
 DC_OPT_COOPERATIVE, DC_OPT_WAIT_LIMIT_US, DC_OPT_TEST_STALL_LMHEAD, DC_OPT_TEST_STALL_STEP = 1, 2, 3, 4
 
 
@@ -130,6 +131,33 @@ class dc_signals_out(C.Structure):
                                           "status")]
 
 
+class dc_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_layers", "max_batch", "n_kv_heads", "max_ctx", "head_dim")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class dc_cache_rows(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("layer", C.c_int32), ("n_layers", C.c_int32), ("dtype", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64 * 5), ("v_stride", C.c_int64 * 5),
+                ("pos", C.c_void_p), ("n", C.c_void_p)]
+
+
+class dc_qk_in(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "n_q_heads", "n_kv_heads", "head_dim")] + \
+               [("eps", C.c_float), ("rope_theta", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p),
+                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("q_gain", C.c_void_p),
+                ("k_gain", C.c_void_p), ("pos", C.c_void_p), ("q_out", C.c_void_p), ("k_out", C.c_void_p),
+                ("q_out_stride", C.c_int64 * 2), ("k_out_stride", C.c_int64 * 2)]
+
+
+class dc_tree_in(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "layer", "dtype", "n_q_heads", "max_rows")] + \
+               [("scale", C.c_float), ("q", C.c_void_p), ("o", C.c_void_p), ("q_stride", C.c_int64 * 3),
+                ("o_stride", C.c_int64 * 3), ("ctx_len", C.c_void_p), ("n_rows", C.c_void_p),
+                ("mask", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("status", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -163,6 +191,12 @@ def load_library(path: str | None = None):
     lib_.dc_select_batched.argtypes = [C.c_void_p, C.c_int32] + [C.c_void_p] * 5 + [C.POINTER(dc_select_out)]
     lib_.dc_set_option.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
     lib_.dc_debug_logits.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
+    lib_.dc_cache_write.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_cache_rows), C.c_void_p]
+    lib_.dc_cache_read.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_cache_rows), C.c_void_p]
+    lib_.dc_qk_norm_rope.argtypes = [C.POINTER(dc_qk_in), C.c_void_p]
+    lib_.dc_tree_attention.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_tree_in), C.c_void_p]
+    lib_.dc_tree_attention_workspace.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_tree_in), C.POINTER(C.c_uint64)]
+    lib_.dc_tree_mask.argtypes = [_I32P, C.c_int32, C.c_int32, C.c_void_p]
     lib_.dc_last_error.argtypes = [C.c_void_p]
     lib_.dc_last_error.restype = C.c_char_p
     for n in EXPORTS:

@@ -1,0 +1,173 @@
+// dc_tree_attention: checks, the split into units, launches.
+#include "tree_attn.cuh"
+
+#include <atomic>
+
+namespace dc {
+namespace {
+
+// Units of one call: stretches of `tiles` tiles of keys, `line_tiles` stretches of lines a sequence.
+struct TreePlan {
+  int lines_per_unit, slots;
+  int tiles, joined, line_tiles;
+  int lines, base[DC_MAX_BATCH];
+  uint64_t bytes;
+};
+
+// The stretch that ends first when `slots` units run at once: a unit costs its tiles and a start (barriers, queries, the first
+// loads' latency, the output), and joining costs a launch; both in the time of a tile.
+constexpr int kUnitStart = 2, kJoin = 2;
+
+TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, int slots) {
+  TreePlan p{};
+  p.lines_per_unit = lines_per_unit; p.slots = slots;
+  const int G = in->n_q_heads / c->n_kv_heads;
+  int longest = 0, units[DC_MAX_BATCH], tiles[DC_MAX_BATCH];
+  for (int b = 0; b < in->batch; ++b) {
+    const int R = in->n_rows[b];
+    p.base[b] = p.lines;
+    p.lines += R * in->n_q_heads;
+    const int lt = (R * G + lines_per_unit - 1) / lines_per_unit;
+    p.line_tiles = p.line_tiles > lt ? p.line_tiles : lt;
+    units[b] = lt * c->n_kv_heads;
+    tiles[b] = R ? (in->ctx_len[b] + R + kTreeTile - 1) / kTreeTile : 0;
+    longest = longest > tiles[b] ? longest : tiles[b];
+  }
+  long long best = -1;
+  for (int s = 1, before = 0; s <= longest && s <= 256; ++s) {
+    const int t = (longest + s - 1) / s;
+    if (t == before) continue;
+    before = t;
+    long long n = 0;
+    for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * ((tiles[b] + t - 1) / t);
+    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (t < longest ? kJoin : 0);
+    if (best < 0 || cost < best) { best = cost; p.tiles = t; }
+  }
+  p.joined = longest ? (longest + p.tiles - 1) / p.tiles : 0;
+  if (p.joined > 1) {
+    const uint64_t n = (uint64_t)p.joined * p.lines;
+    p.bytes = n * 8 + (n & 1) * 8 + n * c->head_dim * 4;
+  }
+  return p;
+}
+
+int sm_count() {
+  // (a property of the device; 148 on a B200)
+  static std::atomic<int> n[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 148; }
+  int v = dev < 64 ? n[dev].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); v = 148; }
+    if (dev < 64) n[dev].store(v, std::memory_order_relaxed);
+  }
+  return v;
+}
+
+TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
+  return make_plan(c, in, kTreeLines, 2 * sm_count());
+}
+
+int check(const dc_cache* c, const dc_tree_in* in) {
+  int rc = op_check_cache(c);
+  if (rc != DC_OK) return rc;
+  if (!in) return op_fail(DC_ERR_INVALID_ARG, "null argument");
+  if ((rc = op_check_dtype(c, in->dtype)) != DC_OK || (rc = op_check_batch(c, in->batch)) != DC_OK) return rc;
+  if (in->layer < 0 || in->layer >= c->n_layers) return op_fail(DC_ERR_SHAPE, "layer %d of %d", in->layer, c->n_layers);
+  if (in->n_q_heads < 1 || in->n_q_heads % c->n_kv_heads)
+    return op_fail(DC_ERR_INVALID_ARG, "%d query heads over %d kv heads", in->n_q_heads, c->n_kv_heads);
+  if (in->max_rows < 1 || in->max_rows > DC_MAX_WINDOW) return op_fail(DC_ERR_SHAPE, "max_rows=%d outside [1, %d]", in->max_rows, (int)DC_MAX_WINDOW);
+  if (!(in->scale >= 0.f) || in->scale > 3e38f) return op_fail(DC_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  if ((rc = op_check_keys(c, in->batch, in->ctx_len, in->n_rows, in->max_rows, ", max_rows bounds the rows")) != DC_OK) return rc;
+  if ((long long)in->max_rows * in->n_q_heads > 524288) return op_fail(DC_ERR_UNSUPPORTED, "more than 524288 rows x query heads");
+  return DC_OK;
+}
+
+// once per device and kernel: shared memory beyond 48 KB
+template <typename K>
+bool opt_in(K kernel, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+  done.fetch_or(bit, std::memory_order_release);
+  return true;
+}
+
+template <typename T, typename H>
+bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
+  static std::atomic<unsigned long long> done;
+  if (!opt_in(k_tree_simt<T, H>, tree_simt_smem(256), done)) return false;
+  k_tree_simt<T, H><<<dim3(p.joined, p.line_tiles * a.c.n_kv_heads, batch), 128, tree_simt_smem(a.c.head_dim), s>>>(a);
+  return true;
+}
+
+}  // namespace
+}  // namespace dc
+
+using namespace dc;
+
+extern "C" int dc_tree_attention_workspace(const dc_cache* cache, const dc_tree_in* in, uint64_t* bytes) {
+  const int rc = check(cache, in);
+  if (rc != DC_OK) return rc;
+  if (!bytes) return op_fail(DC_ERR_INVALID_ARG, "null argument");
+  *bytes = plan(cache, in).bytes;
+  return DC_OK;
+}
+
+extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, void* cuda_stream) {
+  const int rc = check(cache, in);
+  if (rc != DC_OK) return rc;
+  if (!in->q || !in->o) return op_fail(DC_ERR_INVALID_ARG, "null argument");
+  const TreePlan p = plan(cache, in);
+  if (p.lines == 0) return DC_OK;
+  if (p.bytes && (!in->workspace || !op_aligned(in->workspace) || in->workspace_bytes < p.bytes))
+    return op_fail(DC_ERR_INVALID_ARG, "the workspace needs %llu bytes on a 16-byte boundary", (unsigned long long)p.bytes);
+  if ((long long)p.line_tiles * cache->n_kv_heads > 65535) return op_fail(DC_ERR_UNSUPPORTED, "too many kv heads");
+  TreeArgs a;
+  a.c = *cache;
+  const size_t layer = (size_t)in->layer * cache->max_batch * cache->n_kv_heads * cache->max_ctx;   // keys
+  const size_t bytes = layer * cache->head_dim * (cache->dtype == DC_F32 ? 4 : cache->dtype == DC_BF16 ? 2 : 1);
+  a.c.k = static_cast<char*>(cache->k) + bytes; a.c.v = static_cast<char*>(cache->v) + bytes;
+  if (cache->k_scale) { a.c.k_scale += layer; a.c.v_scale += layer; }
+  a.q = in->q; a.o = in->o;
+  for (int i = 0; i < 3; ++i) { a.qs[i] = in->q_stride[i]; a.os[i] = in->o_stride[i]; }
+  a.mask = in->mask; a.max_rows = in->max_rows; a.words = (in->max_rows + 31) / 32;
+  a.nq = in->n_q_heads; a.group = in->n_q_heads / cache->n_kv_heads;
+  a.scale_log2 = (in->scale > 0.f ? in->scale : 1.f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
+  a.tiles = p.tiles; a.joined = p.joined; a.lines = p.lines;
+  for (int b = 0; b < DC_MAX_BATCH; ++b) {
+    a.base[b] = b < in->batch ? p.base[b] : 0;
+    a.ctx[b] = b < in->batch ? in->ctx_len[b] : 0;
+    a.rows[b] = b < in->batch ? in->n_rows[b] : 0;
+  }
+  const uint64_t n = (uint64_t)p.joined * p.lines;
+  a.part_ml = static_cast<float2*>(in->workspace);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(in->workspace) + n * 8 + (n & 1) * 8);
+  a.status = in->status;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
+  const bool ok = f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
+                      : (q8 ? launch_simt<__nv_bfloat16, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<__nv_bfloat16, __nv_bfloat16>(a, p, in->batch, s));
+  if (!ok) return op_fail(DC_ERR_CUDA, "dc_tree_attention: no shared memory");
+  if (p.joined > 1) {
+    const dim3 grid((p.lines + 7) / 8);
+    if (f32) launch_chained(k_tree_join<float>, grid, dim3(256), 0, s, a, in->batch);
+    else launch_chained(k_tree_join<__nv_bfloat16>, grid, dim3(256), 0, s, a, in->batch);
+  }
+  return op_launched("dc_tree_attention");
+}
+
+extern "C" int dc_tree_mask(const int32_t* parent, int32_t n, int32_t words, uint32_t* mask) {
+  if (!parent || !mask) return op_fail(DC_ERR_INVALID_ARG, "null argument");
+  if (n < 0 || n > DC_MAX_WINDOW || words < (n + 31) / 32) return op_fail(DC_ERR_SHAPE, "%d rows with masks of %d words", n, words);
+  for (int r = 0; r < n; ++r)
+    if (parent[r] < -1 || parent[r] >= r) return op_fail(DC_ERR_INVALID_ARG, "parent[%d]=%d is not an earlier row or -1", r, parent[r]);
+  for (int r = 0; r < n; ++r) {
+    uint32_t* m = mask + (size_t)r * words;
+    for (int w = 0; w < words; ++w) m[w] = parent[r] >= 0 ? mask[(size_t)parent[r] * words + w] : 0u;
+    m[r >> 5] |= 1u << (r & 31);
+  }
+  return DC_OK;
+}
