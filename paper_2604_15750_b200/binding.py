@@ -191,11 +191,12 @@ def load_library(path: str | None = None):
     lib_.dc_select_batched.argtypes = [C.c_void_p, C.c_int32] + [C.c_void_p] * 5 + [C.POINTER(dc_select_out)]
     lib_.dc_set_option.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
     lib_.dc_debug_logits.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
-    lib_.dc_cache_write.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_cache_rows), C.c_void_p]
-    lib_.dc_cache_read.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_cache_rows), C.c_void_p]
-    lib_.dc_qk_norm_rope.argtypes = [C.POINTER(dc_qk_in), C.c_void_p]
-    lib_.dc_tree_attention.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_tree_in), C.c_void_p]
-    lib_.dc_tree_attention_workspace.argtypes = [C.POINTER(dc_cache), C.POINTER(dc_tree_in), C.POINTER(C.c_uint64)]
+    # (structures by address: ops.py packs them as bytes, which takes a quarter of the time of filling a Structure)
+    lib_.dc_cache_write.argtypes = [C.c_void_p] * 3
+    lib_.dc_cache_read.argtypes = [C.c_void_p] * 3
+    lib_.dc_qk_norm_rope.argtypes = [C.c_void_p] * 2
+    lib_.dc_tree_attention.argtypes = [C.c_void_p] * 3
+    lib_.dc_tree_attention_workspace.argtypes = [C.c_void_p] * 3
     lib_.dc_tree_mask.argtypes = [_I32P, C.c_int32, C.c_int32, C.c_void_p]
     lib_.dc_last_error.argtypes = [C.c_void_p]
     lib_.dc_last_error.restype = C.c_char_p

@@ -66,6 +66,118 @@ __global__ void __launch_bounds__(kQkThreads) k_qk_any(const __grid_constant__ Q
   }
 }
 
+// head_dim 64, 128 or 256 on 16-byte boundaries: LPH = head_dim / 16 lanes take a head, each 8 pairs (8 dims of the first
+// half, 8 of the second), so that the rotation stays in the lane and the sum of squares takes log2(LPH) shuffles.  A CTA takes a row's
+// heads; their loads are under way while its threads make the row's cos and sin.
+constexpr int kQkVecThreads = 512;
+
+__device__ __forceinline__ void qk_load(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void qk_load(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void qk_store(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void qk_store(__nv_bfloat16* p, const float (&x)[8]) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    u[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kQkVecThreads) k_qk_vec(const __grid_constant__ QkArgs a) {
+  constexpr int LPH = HD / 16, HALF = HD / 2;
+  __shared__ __align__(16) float cs[HALF], sn[HALF];
+  const int c = threadIdx.x % LPH * 8, slots = blockDim.x / LPH, heads = a.heads[0] + a.heads[1], t = blockIdx.x;
+  float u[8], v[8];
+  auto load = [&](int j) {
+    if (j < heads) {
+      const int w = j >= a.heads[0];
+      const T* x = static_cast<const T*>(a.x[w]) + t * a.xs[w][0] + (w ? j - a.heads[0] : j) * a.xs[w][1];
+      qk_load(x + c, u);
+      qk_load(x + HALF + c, v);
+    }
+  };
+  int j = blockIdx.y * slots + threadIdx.x / LPH;
+  load(j);
+  const double p = (double)a.pos[t];
+  for (int i = threadIdx.x; i < HALF; i += blockDim.x) qk_angle(p * a.freq[i], cs[i], sn[i]);
+  __syncthreads();
+  // (every lane stays: the lanes of a head may share a warp with those of a head that is not there)
+  for (int base = blockIdx.y * slots; base < heads; base += gridDim.y * slots, j += gridDim.y * slots) {
+    if (base != (int)blockIdx.y * slots) load(j);
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
+#pragma unroll
+    for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    if (j >= heads) continue;
+    const int w = j >= a.heads[0];
+    const float r = rsqrtf(ss * (1.f / HD) + a.eps);
+    float y0[8], y1[8];
+    if (a.gain[w]) {
+      const T* gain = static_cast<const T*>(a.gain[w]);
+      qk_load(gain + c, y0);
+      qk_load(gain + HALF + c, y1);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { y0[i] *= u[i] * r; y1[i] *= v[i] * r; }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { y0[i] = u[i] * r; y1[i] = v[i] * r; }
+    }
+    float cc[8], ss8[8];
+    qk_load(cs + c, cc);
+    qk_load(sn + c, ss8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = y0[i], p1 = y1[i];
+      y0[i] = p0 * cc[i] - p1 * ss8[i];
+      y1[i] = p1 * cc[i] + p0 * ss8[i];
+    }
+    T* y = static_cast<T*>(a.y[w]) + t * a.ys[w][0] + (w ? j - a.heads[0] : j) * a.ys[w][1];
+    qk_store(y + c, y0);
+    qk_store(y + HALF + c, y1);
+  }
+}
+
+template <typename T, int HD>
+void launch_vec(const QkArgs& a, cudaStream_t s) {
+  constexpr int LPH = HD / 16;
+  const int heads = a.heads[0] + a.heads[1];
+  // Few rows: the heads of a row are spread over CTAs of a warp or more each, as long as there are SMs without work
+  const int spread = max(1, 148 / a.rows);
+  const int threads = min(kQkVecThreads, ((heads + spread - 1) / spread * LPH + 31) / 32 * 32);
+  const int slots = threads / LPH;
+  k_qk_vec<T, HD><<<dim3(a.rows, min((heads + slots - 1) / slots, max(spread, 1))), threads, 0, s>>>(a);
+}
+
+template <typename T>
+bool launch_vec(const QkArgs& a, cudaStream_t s) {
+  constexpr int e16 = 16 / sizeof(T);
+  if (a.hd != 64 && a.hd != 128 && a.hd != 256) return false;
+  for (int w = 0; w < 2; ++w) {
+    if (a.heads[w] == 0) continue;
+    if (!op_aligned(a.x[w]) || !op_aligned(a.y[w]) || !op_aligned(a.gain[w])) return false;
+    for (int i = 0; i < 2; ++i)
+      if (a.xs[w][i] % e16 || a.ys[w][i] % e16) return false;
+  }
+  if (a.hd == 64) launch_vec<T, 64>(a, s);
+  else if (a.hd == 128) launch_vec<T, 128>(a, s);
+  else launch_vec<T, 256>(a, s);
+  return true;
+}
+
 }  // namespace
 }  // namespace dc
 
@@ -91,11 +203,12 @@ extern "C" int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream) {
   const double step = pow((double)in->rope_theta, -2.0 / in->head_dim);
   double f = 1.0;
   for (int i = 0; i < 128; ++i) { a.freq[i] = f; f *= step; }   // (off by at most i roundings of 2^-53)
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (in->dtype == DC_F32 ? launch_vec<float>(a, s) : launch_vec<__nv_bfloat16>(a, s)) return op_launched("dc_qk_norm_rope");
   const int heads = a.heads[0] + a.heads[1];
   const int across = (heads + kQkThreads / 32 - 1) / (kQkThreads / 32);
   // few rows: the heads of a row spread over CTAs
   const dim3 grid(min(in->rows, 1 << 20), min(across, max(1, 296 / min(in->rows, 296))));
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (in->dtype == DC_F32) k_qk_any<float><<<grid, kQkThreads, 0, s>>>(a);
   else k_qk_any<__nv_bfloat16><<<grid, kQkThreads, 0, s>>>(a);
   return op_launched("dc_qk_norm_rope");

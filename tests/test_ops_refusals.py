@@ -150,6 +150,20 @@ def test_masks_of_what_is_no_tree(p):
         dc.tree_mask([[-1, 0]], rows=1)
 
 
+def test_the_packed_structures_are_those_of_the_header():
+    from paper_2604_15750_b200 import ops
+    assert [x.size for x in (ops._CACHE, ops._ROWS, ops._QK, ops._TREE)] == \
+        [C.sizeof(x) for x in (b.dc_cache, b.dc_cache_rows, b.dc_qk_in, b.dc_tree_in)] == [56, 128, 152, 136]
+    for packed, t in ((ops._CACHE, b.dc_cache), (ops._ROWS, b.dc_cache_rows), (ops._QK, b.dc_qk_in), (ops._TREE, b.dc_tree_in)):
+        flat, at = [], 0
+        for name, kind in t._fields_:
+            flat += [(name, i) for i in range(kind._length_)] if hasattr(kind, "_length_") else [(name, None)]
+        s = t.from_buffer_copy(packed.pack(*range(1, len(flat) + 1)))
+        for i, (name, j) in enumerate(flat):
+            v = getattr(s, name)
+            assert (v if j is None else v[j]) == i + 1, name
+
+
 # ---- the binding ------------------------------------------------------------------------------------------
 def _kv(dtype=torch.bfloat16, hd=128):
     return torch.zeros((1, 2, 2, 64, hd), dtype=dtype), torch.zeros((1, 2, 2, hd, 64), dtype=dtype)
