@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "ops.h"
 #include "simt_step.h"
 #include "tc.h"
 
@@ -936,8 +937,9 @@ int dc_set_option(dc_ctx* c, int32_t option, int32_t value) {
   }
   if (option == DC_OPT_WAIT_LIMIT_US) {
     if (value < 1000 || value > 60000000) return fail(c, DC_ERR_INVALID_ARG, "wait limit outside [1000, 60000000] us");
-    // (the tensor-core kernels and the fused CUDA-core step have a word each on the device)
-    if (simt_set_wait_limit_us(value, c->stream) != 0 || tc_set_wait_limit_us(value, c->stream) != 0) {
+    // (the tensor-core kernels, the fused CUDA-core step and the attention of drafted rows have a word each on the device)
+    if (simt_set_wait_limit_us(value, c->stream) != 0 || tc_set_wait_limit_us(value, c->stream) != 0 ||
+        tree_set_wait_limit_us(value, c->stream) != 0) {
       cudaGetLastError();
       return fail(c, DC_ERR_CUDA, "setting the wait limit failed");
     }

@@ -61,6 +61,9 @@ inline int op_check_keys(const dc_cache* c, int batch, const int32_t* first, con
 
 inline bool op_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// DC_OPT_WAIT_LIMIT_US for the waits of dc_tree_attention's kernel; 0 or a CUDA error
+int tree_set_wait_limit_us(long long us, cudaStream_t s);
+
 // ---- types --------------------------------------------------------------------------------------------
 __device__ __forceinline__ float op_f32(float x) { return x; }
 __device__ __forceinline__ float op_f32(__nv_bfloat16 x) { return __bfloat162float(x); }

@@ -79,6 +79,23 @@ bool make_map_heads(CUtensorMap* m, const void* base, uint64_t heads, uint64_t K
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+}  // namespace
+
+// 2-D row-major [rows, cols] tensor of bf16 or of bytes: a box is 128 bytes of a row x 128 rows, swizzled and filled as above
+bool tc_map_bytes(CUtensorMap* m, const void* base, int element_bytes, uint64_t rows, uint64_t cols) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols * element_bytes};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / element_bytes), 128};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(m, element_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
+             box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
 constexpr int kSmemBudget = 232448 - 1024;  // opt-in shared memory per CTA, minus alignment slack
 constexpr int kGemmStatic = 512;            // static shared memory of k_gemm_tc (upper bound)
 

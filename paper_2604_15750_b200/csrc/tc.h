@@ -1,5 +1,7 @@
 // Tensor-core (tcgen05 + TMA) half of the block-step: dense layers, attention, LM head.
 #pragma once
+#include <cuda.h>
+
 #include <vector>
 
 #include "kernels.h"
@@ -17,6 +19,9 @@ struct TcState;
 
 // phases of the persistent dense chain, in execution order
 enum { CH_OPROJ = 0, CH_NORM2 = 1, CH_GATEUP = 2, CH_DOWN = 3, CH_NORM1 = 4, CH_QKV = 5, CH_END = 6 };
+
+// tensor map of a cache array of one layer, [rows, cols] of 2- or 1-byte elements (tc_tree.cuh)
+bool tc_map_bytes(CUtensorMap* m, const void* base, int element_bytes, uint64_t rows, uint64_t cols);
 
 // true if the tensor-core kernels take this model shape
 bool tc_supported(const dc_config& g);

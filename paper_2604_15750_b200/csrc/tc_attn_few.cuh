@@ -57,22 +57,6 @@ struct FewCtl {
 };
 static_assert(sizeof(FewCtl) <= 1024, "control block");
 
-// Reduces v[row] over the lanes of a warp, all 32 rows at once: lane i returns row i's result.
-template <bool MAX>
-__device__ __forceinline__ float few_reduce(float (&v)[32], int lane) {
-#pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) {
-    const bool upper = (lane & s) != 0;
-#pragma unroll
-    for (int i = 0; i < s; ++i) {
-      const float send = upper ? v[i] : v[i + s], keep = upper ? v[i + s] : v[i];
-      const float got = __shfl_xor_sync(0xffffffffu, send, s);
-      v[i] = MAX ? fmaxf(keep, got) : keep + got;
-    }
-  }
-  return v[0];
-}
-
 __global__ void __launch_bounds__(kFewThreads, 2)
 k_attn_few(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
            const __grid_constant__ CUtensorMap map_vt, const __grid_constant__ CUtensorMap map_kc,

@@ -1,0 +1,551 @@
+// dc_tree_attention on tcgen05: bf16 rows, head_dim 128, a cache of bf16 or e4m3.  Keys on the 128 lanes, lines (tree_attn.cuh)
+// on N columns, as in tc_attn_few.cuh:
+//
+//   S^T [128 keys x N lines]  = K Q^T
+//   P^T                       = 2^(t - m),   t = scale * log2(e) * S     (0 where a line does not see the key)
+//   O^T [128 dims x N lines] += V^T P^T      sums l += P^T over the keys beside it
+//
+// Few lines stream many keys: the cache's bytes are the bound (64 KB of bf16 or 32 KB of e4m3 a tile of 128 keys; at
+// 6.5 TB/s an SM gets one in 2800 or 1400 clocks), and one thread per key does the softmax of N lines in less.
+//
+// An e4m3 cache goes to the tensor cores as it is (kind::f8f6f4), no byte of it is converted.  The other operand must be
+// e4m3 too, and one e4m3 number has 4 significant bits, so it is given as the sum of two:
+//   q = 2^e (hi + lo): 4 + 4 bits hold the 8 of a bf16 value exactly (per line, largest magnitude in [128, 256); what is
+//     2^10 below that is off by 2^-18 of it at most); both products go to the same accumulator
+//   P' = 2^(t + log2 v_scale + 4 - m) = hi + lo / 16: 8 bits, not finer than 2^-14 where the largest is 16 .. 256; two accumulators
+// The scales are factors of a key, and a thread has one key: K's goes into t, V's into P', so that the sum of a line
+// takes P' / (16 v_scale).  The maximum m is that of t + log2 v_scale.
+//
+// m of a line is the maximum of the first tile that it sees and moves only when a later tile has a t above it by more than kHead
+// (a vote of the four warps that hold a line's keys): then O and the sums are scaled by 2^(m_old - m_new).
+//
+// Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, 3 = puts V^T tiles in order
+// (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
+// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every 32 lines.
+#pragma once
+#include "tc_attn_parts.cuh"
+#include "tree_attn.cuh"
+
+namespace dc {
+
+template <int N, bool Q8>
+struct TreeTc {
+  static constexpr int kThreads = 128 + 4 * N;                 // four warps for every 32 lines
+  static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
+  static constexpr int kRing = Q8 ? (N == 32 ? 2 : 4) : 3;     // slots of each ring
+  static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
+  static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
+  static constexpr int kCtl = 3072;
+  static constexpr int kSmem = 2 * kOperand + 2 * kRing * kSlot + kCtl;
+  static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : 256;   // TMEM: S^T twice, O^T (its two parts)
+};
+constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.f;   // (P' = 2^(4 + 4) at most: e4m3 ends at 448)
+
+template <int N>
+struct TreeCtl {
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full, p_empty;
+  uint32_t tmem_base;
+  int abort_flag, late_flag;
+  uint32_t poison[8];                    // drafted keys whose V is not finite
+  alignas(16) float m[2][N];             // the lines' maxima (log2 units), the current set and the one before
+  alignas(16) float rs[N];               // e4m3: 2^e of a line's q
+  float part[4][N];
+  alignas(16) float inv[N];
+};
+
+// D (+)= A B with e4m3 operands, 32 deep (split descriptors as umma_bf16_lo)
+__device__ __forceinline__ void tree_umma_f8(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
+      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// e4m3 x e4m3 -> fp32, both K-major
+__device__ __forceinline__ uint32_t tree_idesc_f8(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
+
+__device__ __forceinline__ uint32_t tree_e4m3x2(float x0, float x1) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ float2 tree_from_e4m3x2(uint32_t u) {
+  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)u, __NV_E4M3)));
+}
+
+// Queries of a CTA's lines into shared memory, rows of 128 bytes with the 128-byte swizzle; e4m3: hi, then lo.  VEC: 16-byte loads.
+template <int N, bool Q8, bool VEC>
+__device__ __forceinline__ void tree_queries(const TreeArgs& a, int b, int g, int line0, int n, uint8_t* Qs, float* rs) {
+  for (int i = threadIdx.x; i < N * 16; i += TreeTc<N, Q8>::kThreads) {   // (N * 16 and the threads are whole warps)
+    const int line = i >> 4, c = i & 15, m = line0 + line;      // 8 dims of a line
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (line < n) {
+      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + b * a.qs[0] + (m / a.group) * a.qs[1] + (g * a.group + m % a.group) * a.qs[2] + c * 8;
+      if (VEC) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__bfloat16_as_ushort(q[2 * e]) | (uint32_t)__bfloat16_as_ushort(q[2 * e + 1]) << 16;
+      }
+    }
+    if (!Q8) {
+      *reinterpret_cast<uint4*>(Qs + (c >> 3) * (N * 128) + line * 128 + (((c & 7) ^ (line & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      uint32_t top = 0;     // magnitudes order as their patterns do
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+#pragma unroll
+      for (int s = 8; s >= 1; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+      const int ex = max((int)(top >> 7), 20) - 127;            // of the largest magnitude
+      const float f = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+      if (c == 0) rs[line] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)(127 - 7 + ex) << 23);
+      uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
+        const uint32_t h = tree_e4m3x2(x0, x1);
+        const float2 r = tree_from_e4m3x2(h);
+        hi[e >> 1] |= h << (16 * (e & 1));
+        lo[e >> 1] |= tree_e4m3x2(x0 - r.x, x1 - r.y) << (16 * (e & 1));
+      }
+      uint8_t* at = Qs + line * 128 + (((c >> 1) ^ (line & 7)) << 4) + (c & 1) * 8;
+      *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(at + N * 128) = make_uint2(lo[0], lo[1]);
+    }
+  }
+}
+
+// Address of the 16-byte piece of row rr of a V^T tile: pieces of 16 (e4m3) or 8 keys
+template <bool Q8>
+__device__ __forceinline__ uint4* tree_v_piece(uint8_t* tile, int rr, int piece) {
+  if (Q8) return reinterpret_cast<uint4*>(tile + rr * 128 + ((piece ^ (rr & 7)) << 4));
+  return reinterpret_cast<uint4*>(tile + (piece >> 3) * kSub + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4));
+}
+
+// Values of drafted keys (in the tile: from .. to - 1) that are not finite: cleared, and their keys noted
+template <bool Q8>
+__device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison) {
+  constexpr int KPP = Q8 ? 16 : 8, KPW = Q8 ? 4 : 2;     // keys of a piece, of a word
+  const int lane = threadIdx.x & 31;
+  for (int pc = from / KPP; pc * KPP < to; ++pc)
+    for (int rr = lane; rr < 128; rr += 32) {
+      uint4* at = tree_v_piece<Q8>(tile, rr, pc);
+      uint4 w4 = *at;
+      uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t bad = Q8 ? ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w[i] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+        if (bad) {
+#pragma unroll
+          for (int e = 0; e < KPW; ++e) {
+            const int key = pc * KPP + i * KPW + e;
+            if (((bad >> (e * (32 / KPW))) & (Q8 ? 0xffu : 0xffffu)) && key >= from && key < to) {
+              w[i] &= ~((Q8 ? 0xffu : 0xffffu) << (e * (32 / KPW)));
+              const int j = key - from + first_draft;
+              atomicOr(&poison[j >> 5], 1u << (j & 31));
+              any = true;
+            }
+          }
+        }
+      }
+      if (any) *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Clears keys valid .. up to what the product takes (its steps are 32 keys of e4m3) in row rr
+__device__ __forceinline__ void tree_clear_v8(uint8_t* tile, int rr, int valid) {
+  const int c = valid >> 4, k = valid & 15;
+  uint4* at = tree_v_piece<true>(tile, rr, c);
+  uint4 w = *at;
+  auto kept = [&](int first) { const int n = k - first; return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; };
+  w.x &= kept(0); w.y &= kept(4); w.z &= kept(8); w.w &= kept(12);
+  *at = w;
+  if ((c & 1) == 0) *tree_v_piece<true>(tile, rr, c + 1) = make_uint4(0, 0, 0, 0);
+}
+
+template <int N, bool Q8>
+__global__ void __launch_bounds__(TreeTc<N, Q8>::kThreads, TreeTc<N, Q8>::kResident)
+k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a, const int vec_q) {
+  using C = TreeTc<N, Q8>;
+  extern __shared__ uint8_t smem_tree[];
+  const int b = blockIdx.z, R = a.rows[b], G = a.group, nkv = a.c.n_kv_heads;
+  const int g = blockIdx.y % nkv, line0 = blockIdx.y / nkv * N, n = min(N, R * G - line0);
+  const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
+  const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
+  if (n <= 0 || T <= 0) return;
+  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRing * C::kSlot;
+  TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRing * C::kSlot);
+  static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((ptx::smem_u32(smem_tree) & 1023u) != 0) {   // (it is all the shared memory there is and starts on such a boundary)
+    if (threadIdx.x == 0 && a.status) atomicExch(a.status, DC_ERR_UNSUPPORTED);
+    return;
+  }
+
+  if (threadIdx.x == 0) {
+    c.abort_flag = 0; c.late_flag = 0;
+    for (int i = 0; i < C::kRing; ++i) {
+      ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1);
+      ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], N / 8); }
+    ptx::mbar_init(&c.p_full, N / 8 + 1);   // the softmax warps, and warp 3
+    ptx::mbar_init(&c.p_empty, 1);
+    ptx::fence_barrier_init();
+  }
+  if (threadIdx.x < 8) c.poison[threadIdx.x] = 0u;
+  if (threadIdx.x < N) c.m[0][threadIdx.x] = (int)threadIdx.x < n ? -INFINITY : INFINITY;   // (columns without a line: P = 0)
+  if (warp == 1) {
+    ptx::tmem_alloc(&c.tmem_base, C::kCols);
+    ptx::tmem_relinquish();
+  }
+  if (vec_q) tree_queries<N, Q8, true>(a, b, g, line0, n, Qs, c.rs);
+  else tree_queries<N, Q8, false>(a, b, g, line0, n, Qs, c.rs);
+  ptx::fence_proxy_async_smem();
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = c.tmem_base;
+  pdl_trigger();   // (the join; not before the allocation: pdl.cuh)
+
+  int* abort_flag = &c.abort_flag;
+  int loads = 0;   // of the producer thread: tiles of K and of V^T, in turn
+  auto valid_keys = [&](int j) { return min(kTreeTile, keys - (tile0 + j) * kTreeTile); };
+  if (warp == 0) {
+    if (lane == 0) {
+      // ---------------- TMA producer ----------------
+      const int krow = (b * nkv + g) * a.c.max_ctx, vrow = (b * nkv + g) * kHd;
+      for (int j = 0; j < T; ++j) {
+        const int s = j % C::kRing, key = (tile0 + j) * kTreeTile;
+        const uint32_t ph = (uint32_t)(j / C::kRing) & 1u;
+        if (!ptx::mbar_wait(&c.k_empty[s], ph ^ 1u, abort_flag)) break;
+        uint8_t* dst = kring + (size_t)s * C::kSlot;
+        ptx::mbar_expect_tx(&c.k_full[s], C::kSlot);
+        ptx::tma_load_2d(dst, &map_k, &c.k_full[s], 0, krow + key);
+        if (!Q8) ptx::tma_load_2d(dst + kSub, &map_k, &c.k_full[s], 64, krow + key);
+        ++loads;
+        if (!ptx::mbar_wait(&c.v_empty[s], ph ^ 1u, abort_flag)) break;
+        dst = vring + (size_t)s * C::kSlot;
+        ptx::mbar_expect_tx(&c.v_full[s], C::kSlot);
+        ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
+        if (!Q8) ptx::tma_load_2d(dst + kSub, &map_v, &c.v_full[s], key + 64, vrow);
+        ++loads;
+      }
+    }
+  } else if (warp == 1 || warp == 2) {
+    // ---------------- issuers of S^T = K Q^T (warp 1) and O^T (+)= V^T P^T (warp 2) ----------------
+    const bool pv = warp == 2;
+    const uint32_t idesc = Q8 ? tree_idesc_f8(N) : ptx::idesc_bf16(128, N), hi32 = ptx::smem_desc_hi32();
+    const uint32_t b_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs)), ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
+    bool ok = true;
+    for (int j = 0; j < T && ok; ++j) {
+      const int s = j % C::kRing;
+      if (pv) ok = ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
+      else if (j >= 2) ok = ptx::mbar_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
+      ok = ok && ptx::mbar_wait(pv ? &c.v_full[s] : &c.k_full[s], (uint32_t)(j / C::kRing) & 1u, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      if (ptx::elect_one()) {
+        const uint32_t d = tmem_base + (pv ? (uint32_t)C::kColO : (uint32_t)(j & 1) * N);
+        const uint32_t t = ring_lo + (uint32_t)s * (C::kSlot >> 4);
+        if (Q8) {
+          const int nk = pv ? (valid_keys(j) + 31) >> 5 : 4;
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              if (kk >= nk) break;
+              tree_umma_f8(pv ? d + part * N : d, t + kk * 2, b_lo + part * (N * 128 >> 4) + kk * 2, hi32, idesc,
+                           (kk > 0 || (pv ? j > 0 : part > 0)) ? 1u : 0u);
+            }
+        } else {
+          const int nk = pv ? attn_pv_keys(valid_keys(j)) >> 4 : 8;
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) {
+            if (kk >= nk) break;
+            const uint32_t k4 = (uint32_t)(kk & 3) * 2u, half = (uint32_t)(kk >> 2);
+            ptx::umma_bf16_lo(d, t + half * (kSub >> 4) + k4, b_lo + half * (N * 128 >> 4) + k4, hi32, idesc, (kk > 0 || (pv && j > 0)) ? 1u : 0u);
+          }
+        }
+        ptx::umma_commit(pv ? &c.v_empty[s] : &c.k_empty[s]);
+        ptx::umma_commit(pv ? &c.p_empty : &c.s_full[j & 1]);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 3) {
+    // ---------------- V^T tiles: beyond the valid keys, and drafted values that are not finite ----------------
+    for (int j = 0; j < T; ++j) {
+      const int s = j % C::kRing, key0 = (tile0 + j) * kTreeTile, valid = valid_keys(j);
+      const bool ragged = (valid & (Q8 ? 31 : 15)) != 0, drafted = a.mask && key0 + valid > ctx;
+      if (ragged || drafted) {
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait(&c.v_full[s], (uint32_t)(j / C::kRing) & 1u, abort_flag))) break;
+        uint8_t* tile = vring + (size_t)s * C::kSlot;
+        if (ragged)
+          for (int rr = lane; rr < 128; rr += 32) {
+            if (Q8) tree_clear_v8(tile, rr, valid);
+            else attn_clear_v(tile, rr, valid);
+          }
+        if (drafted) tree_clean_v<Q8>(tile, max(0, ctx - key0), valid, max(0, key0 - ctx), c.poison);
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+      }
+      if (lane == 0) ptx::mbar_arrive(&c.p_full);
+      // (not ahead of the tile: its next arrival belongs to the next phase)
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag))) break;
+    }
+  } else {
+    // ---------------- softmax: one thread per key of the tile, 32 lines ----------------
+    const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * 32;
+    const int ng = min(32, n - col0);               // lines of this group (0 and less: none)
+    const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
+    const int bar = 1 + group;                      // named barrier of the group's four warps
+    // who sees this thread's key, a bit for each line: tiles without drafted keys by the keys' number alone, the (at most
+    // three) others by the mask
+    const int draft0 = ctx / kTreeTile;
+    uint32_t seen[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int tile = draft0 + i, jd = tile * kTreeTile + key - ctx;
+      seen[i] = jd < R ? 0xffffffffu : 0u;
+      if (a.mask && jd >= 0 && jd < R && tile >= tile0 && tile < tile0 + T) {
+        const uint32_t* col = a.mask + (size_t)b * a.max_rows * a.words + (jd >> 5);
+        uint32_t w = 0;
+        int r = (line0 + col0) / G, left = G - (line0 + col0) % G;    // lines left of row r
+#pragma unroll 8
+        for (int e = 0; e < ng; ++e) {
+          w |= ((col[(size_t)r * a.words] >> (jd & 31)) & 1u) << e;
+          if (--left == 0) { ++r; left = G; }
+        }
+        seen[i] = w;
+      }
+    }
+    const float* k_scale = nullptr;
+    const float* v_scale = nullptr;
+    float ks = 0.f, vs = 1.f;      // of this thread's key in the tile to come
+    if (Q8) {
+      const size_t at = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + key;
+      k_scale = a.c.k_scale + at; v_scale = a.c.v_scale + at;
+      if (key < valid_keys(0)) { ks = k_scale[0]; vs = v_scale[0]; }
+    }
+    // this key's place in P (bf16: rows of 64 keys, two halves; e4m3: rows of 128), lines 8 i + e at 1024 i from that of line e
+    uint32_t p_addr[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t base = ptx::smem_u32(Ps) + (uint32_t)(col0 * 128 + e * 128);
+      p_addr[e] = Q8 ? base + (uint32_t)((((key >> 4) ^ e) << 4) + (key & 15))
+                     : base + (uint32_t)((key >> 6) * (N * 128) + ((((key & 63) >> 3) ^ e) << 4) + (key & 7) * 2);
+    }
+    float acc[32];   // the lines' sums over this thread's keys
+#pragma unroll
+    for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+    int cur = 0;
+    bool ok = true;
+    for (int j = 0; j < T; ++j) {
+      const int tile = tile0 + j, d = tile - draft0;
+      uint32_t sees = d < 0 ? 0xffffffffu : d == 0 ? seen[0] : d == 1 ? seen[1] : seen[2];
+      const float mul = Q8 ? ks * a.scale_log2 : a.scale_log2;
+      // (a row of zeros may come with a scale of 0: it counts in the sum)
+      const float v_sc = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;   // 2^-100
+      const float lv = Q8 ? __log2f(v_sc) : 0.f, iv = Q8 && v_sc <= 3.402823466e38f ? __frcp_rn(v_sc * 16.f) : 0.f;
+      if (Q8 && j + 1 < T && key < valid_keys(j + 1)) { ks = k_scale[(size_t)(j + 1) * kTreeTile]; vs = v_scale[(size_t)(j + 1) * kTreeTile]; }
+      ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag));
+      // (whatever their waits said, the four warps of a group come to its barriers together)
+      ok = ptx::all_agree(bar, 128, ok);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
+      float v[32];
+      for (int turn = 0; turn < 2; ++turn) {
+        ptx::tmem_ld_32x32(s_col, v);
+        ptx::tmem_ld_wait();
+        float most = -INFINITY;
+        const float off = Q8 ? lv + 4.f : 0.f;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          if (e >= ng) break;
+#pragma unroll
+          for (int i = e; i < e + 8; i += 4) {
+            const float4 m4 = *reinterpret_cast<const float4*>(&c.m[cur][col0 + i]);
+            if (Q8) {
+              const float4 r4 = *reinterpret_cast<const float4*>(&c.rs[col0 + i]);
+              v[i] *= r4.x; v[i + 1] *= r4.y; v[i + 2] *= r4.z; v[i + 3] *= r4.w;
+            }
+            v[i] = fmaf(v[i], mul, off - m4.x);
+            v[i + 1] = fmaf(v[i + 1], mul, off - m4.y);
+            v[i + 2] = fmaf(v[i + 2], mul, off - m4.z);
+            v[i + 3] = fmaf(v[i + 3], mul, off - m4.w);
+          }
+          if (sees != 0xffffffffu) {
+#pragma unroll
+            for (int i = e; i < e + 8; ++i) v[i] = (sees >> i) & 1u ? v[i] : -INFINITY;
+          }
+#pragma unroll
+          for (int i = e; i < e + 8; i += 2) most = ptx::fmax3(most, v[i], v[i + 1]);
+        }
+        if (turn == 1 || ptx::all_agree(bar, 128, !(most > (Q8 ? kHeadE4m3 : kHeadBf16)))) break;
+        // ---- the maxima move: from the scores themselves, over the group's four warps ----
+        ptx::tmem_ld_32x32(s_col, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float u = fmaf(Q8 ? v[i] * c.rs[col0 + i] : v[i], mul, lv);
+          v[i] = i < ng && ((sees >> i) & 1u) ? u : -INFINITY;
+        }
+        c.part[quarter][col0 + lane] = few_reduce<true>(v, lane);
+        asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
+        const int col = col0 + lane;
+        const float old = c.m[cur][col];
+        const float now = fmaxf(fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col])), old);
+        const float f = old == -INFINITY ? 0.f : exp2f(old - now);
+        if (quarter == 0) c.m[cur ^ 1][col] = now;
+        if (j > 0) {   // O^T: all products so far are in
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+        }
+        ok = ptx::all_agree(bar, 128, ok);
+        cur ^= 1;
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[i] *= __shfl_sync(0xffffffffu, f, i);
+        if (j > 0) {
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int part = 0; part < (Q8 ? 2 : 1); ++part)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t at = t_lane + (uint32_t)(C::kColO + part * N + half * 16);
+              float o[16];
+              ptx::tmem_ld_32x16(at, o);
+              ptx::tmem_ld_wait();
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * __shfl_sync(0xffffffffu, f, half * 16 + i));
+              attn_tmem_st16(at, w);
+            }
+          ptx::tmem_st_wait();
+          ptx::tc_fence_before();
+        }
+      }
+      if (!ok) break;
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&c.s_empty[j & 1]);
+      if (!Q8) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          if (e >= ng) break;
+#pragma unroll
+          for (int i = e; i < e + 8; ++i) { v[i] = attn_ex2(v[i]); acc[i] += v[i]; }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          if (e >= ng) break;
+#pragma unroll
+          for (int i = e; i < e + 8; ++i) { v[i] = attn_ex2(v[i]); acc[i] = fmaf(v[i], iv, acc[i]); }
+        }
+      }
+      // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
+      if (j > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+      if (!ok) continue;
+#pragma unroll
+      for (int e = 0; e < 32; e += 8) {
+        if (e >= ng) break;
+        if (!Q8) {
+#pragma unroll
+          for (int i = e; i < e + 8; ++i)
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_addr[i & 7] + (uint32_t)(i >> 3) * 1024u),
+                         "h"(__bfloat16_as_ushort(__float2bfloat16_rn(v[i]))) : "memory");
+        } else {
+#pragma unroll
+          for (int i = e; i < e + 8; i += 2) {
+            // hi: the value rounded, lo: 16 times the rest
+            const uint32_t hi = tree_e4m3x2(v[i], v[i + 1]);
+            const float2 r = tree_from_e4m3x2(hi);
+            const uint32_t lo = tree_e4m3x2((v[i] - r.x) * 16.f, (v[i + 1] - r.y) * 16.f);
+            const uint32_t a0 = p_addr[i & 7] + (uint32_t)(i >> 3) * 1024u, a1 = p_addr[(i + 1) & 7] + (uint32_t)(i >> 3) * 1024u;
+            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a0), "r"(hi) : "memory");
+            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a1), "r"(hi >> 8) : "memory");
+            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a0 + N * 128), "r"(lo) : "memory");
+            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a1 + N * 128), "r"(lo >> 8) : "memory");
+          }
+        }
+      }
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&c.p_full);
+    }
+    // O^T is complete once the last P has been read
+    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag));
+    c.part[quarter][col0 + lane] = few_reduce<false>(acc, lane);
+    if (quarter == 0) c.inv[col0 + lane] = c.m[cur][col0 + lane];     // (for the output below)
+  }
+  // ---------------- output ----------------
+  __syncthreads();
+  const bool failed = c.abort_flag != 0, alone = tree_stretches(a, b) == 1;
+  if (warp >= 4) {
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * 32, ng = min(32, n - col0);
+    if (ng > 0) {
+      float o[32];
+      if (!failed) {
+        const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
+        ptx::tc_fence_after();
+        ptx::tmem_ld_32x32(at, o);
+        ptx::tmem_ld_wait();
+        if (Q8) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float lo[16];
+            ptx::tmem_ld_32x16(at + (uint32_t)(N + half * 16), lo);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[half * 16 + i] = fmaf(lo[i], 1.f / 16.f, o[half * 16 + i]) * (1.f / 16.f);
+          }
+        }
+      }
+      // lane = line: its sum, whether it sees a key that is not finite, its place
+      float l = 0.f;
+      if (lane < ng) {
+        const int col = col0 + lane, m = line0 + col, r = m / G, h = g * G + m % G;
+        l = (c.part[0][col] + c.part[1][col]) + (c.part[2][col] + c.part[3][col]);
+        bool bad = failed;
+        if (a.mask)
+          for (int w = 0; w < a.words; ++w)
+            if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
+        if (bad) l = __uint_as_float(0x7fffffffu);
+        if (!alone && quarter == 0)
+          a.part_ml[(size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)] = make_float2(c.inv[col], l);
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
+      int r = (line0 + col0) / G, i_in = (line0 + col0) % G;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (i >= ng) break;
+        const float w = __shfl_sync(0xffffffffu, inv, i);
+        const int h = g * G + i_in, dim = quarter * 32 + lane;
+        if (alone)
+          static_cast<__nv_bfloat16*>(a.o)[b * a.os[0] + r * a.os[1] + h * a.os[2] + dim] = __float2bfloat16_rn(w == 0.f ? 0.f : o[i] * w);
+        else
+          a.part_o[((size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)) * kHd + dim] = o[i];
+        if (++i_in == G) { i_in = 0; ++r; }
+      }
+    }
+  }
+  if (loads > 0 && c.abort_flag != 0) {
+    // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)
+    for (int it = max(0, loads - 2 * C::kRing); it < loads; ++it) {
+      const int j = it >> 1;
+      ptx::mbar_wait((it & 1) == 0 ? &c.k_full[j % C::kRing] : &c.v_full[j % C::kRing], (uint32_t)(j / C::kRing) & 1u, &c.late_flag);
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem_base, C::kCols);
+  }
+  if (threadIdx.x == 0 && c.abort_flag && a.status) atomicExch(a.status, DC_ERR_TIMEOUT);
+}
+
+}  // namespace dc

@@ -1,5 +1,6 @@
 // dc_tree_attention: checks, the split into units, launches.
-#include "tree_attn.cuh"
+#include "tc.h"
+#include "tc_tree.cuh"
 
 #include <atomic>
 
@@ -64,8 +65,19 @@ int sm_count() {
   return v;
 }
 
+// The tensor-core kernel's shapes: N lines of a unit, 0 for the CUDA-core kernel
+int tc_lines(const dc_cache* c, const dc_tree_in* in) {
+  const uint64_t keys = (uint64_t)c->max_batch * c->n_kv_heads * c->max_ctx, dims = (uint64_t)c->max_batch * c->n_kv_heads * kHd;
+  if (in->dtype != DC_BF16 || c->head_dim != kHd || !op_aligned(c->k) || !op_aligned(c->v) || keys >> 31 || dims >> 31) return 0;
+  int most = 0;
+  for (int b = 0; b < in->batch; ++b) most = most > in->n_rows[b] ? most : in->n_rows[b];
+  return most * (in->n_q_heads / c->n_kv_heads) <= 32 ? 32 : 64;
+}
+
 TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
-  return make_plan(c, in, kTreeLines, 2 * sm_count());
+  const int n = tc_lines(c, in);
+  if (n == 0) return make_plan(c, in, kTreeLines, 2 * sm_count());
+  return make_plan(c, in, n, (n == 32 && c->dtype == DC_E4M3 ? 2 : 1) * sm_count());
 }
 
 int check(const dc_cache* c, const dc_tree_in* in) {
@@ -103,7 +115,27 @@ bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s
   return true;
 }
 
+template <int N, bool Q8>
+bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, cudaStream_t s) {
+  using C = TreeTc<N, Q8>;
+  static std::atomic<unsigned long long> done;
+  if (!opt_in(k_tree_tc<N, Q8>, C::kSmem, done)) return false;
+  CUtensorMap mk, mv;
+  const uint64_t heads = (uint64_t)a.c.max_batch * a.c.n_kv_heads;
+  if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
+  k_tree_tc<N, Q8><<<dim3(p.joined, p.line_tiles * a.c.n_kv_heads, batch), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q);
+  return true;
+}
+
 }  // namespace
+
+int tree_set_wait_limit_us(long long us, cudaStream_t s) {
+  const unsigned long long ns = (unsigned long long)us * 1000ull;
+  cudaError_t e = cudaMemcpyToSymbolAsync(ptx::g_wait_limit_ns, &ns, sizeof(ns), 0, cudaMemcpyHostToDevice, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  return (int)e;
+}
+
 }  // namespace dc
 
 using namespace dc;
@@ -148,9 +180,14 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.status = in->status;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
-  const bool ok = f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
+  const int n_lines = p.lines_per_unit == kTreeLines ? 0 : p.lines_per_unit;
+  int vec_q = op_aligned(in->q);
+  for (int i = 0; i < 3; ++i) vec_q = vec_q && in->q_stride[i] % 8 == 0;
+  const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, s) : launch_tc<32, false>(a, p, in->batch, vec_q, s))
+                : n_lines == 64 ? (q8 ? launch_tc<64, true>(a, p, in->batch, vec_q, s) : launch_tc<64, false>(a, p, in->batch, vec_q, s))
+                : f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
                       : (q8 ? launch_simt<__nv_bfloat16, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<__nv_bfloat16, __nv_bfloat16>(a, p, in->batch, s));
-  if (!ok) return op_fail(DC_ERR_CUDA, "dc_tree_attention: no shared memory");
+  if (!ok) return op_fail(DC_ERR_CUDA, "dc_tree_attention: no shared memory or tensor map");
   if (p.joined > 1) {
     const dim3 grid((p.lines + 7) / 8);
     if (f32) launch_chained(k_tree_join<float>, grid, dim3(256), 0, s, a, in->batch);
