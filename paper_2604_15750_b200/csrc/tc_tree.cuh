@@ -19,24 +19,30 @@
 // m of a line is the maximum of the first tile that it sees and moves only when a later tile has a t above it by more than kHead
 // (a vote of the four warps that hold a line's keys): then O and the sums are scaled by 2^(m_old - m_new).
 //
+// P lies in shared memory as the threads have it, a row of N values for a key (the product takes it with the lines as the
+// contiguous axis): a thread stores 16 bytes at a time, where rows of keys would take a store for every value.
+//
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, 3 = puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
-// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every 32 lines.
+// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every kTreeCols lines.
 #pragma once
 #include "tc_attn_parts.cuh"
 #include "tree_attn.cuh"
 
 namespace dc {
 
+constexpr int kTreeCols = 16;    // lines of a softmax warp
+
 template <int N, bool Q8>
 struct TreeTc {
-  static constexpr int kThreads = 128 + 4 * N;                 // four warps for every 32 lines
+  static constexpr int kGroups = N / kTreeCols, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
   static constexpr int kRing = Q8 ? (N == 32 ? 2 : 4) : 3;     // slots of each ring
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
   static constexpr int kCtl = 3072;
   static constexpr int kSmem = 2 * kOperand + 2 * kRing * kSlot + kCtl;
+  static constexpr int kPRow = Q8 ? N : 2 * N;                  // bytes of a key's row of P (of its hi or lo part): 32, 64 or 128
   static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : 256;   // TMEM: S^T twice, O^T (its two parts)
 };
 constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.f;   // (P' = 2^(4 + 4) at most: e4m3 ends at 448)
@@ -47,29 +53,70 @@ struct TreeCtl {
   uint32_t tmem_base;
   int abort_flag, late_flag;
   uint32_t poison[8];                    // drafted keys whose V is not finite
-  alignas(16) float m[2][N];             // the lines' maxima (log2 units), the current set and the one before
+  alignas(16) float nm[2][N];            // the lines' maxima, negative (log2 units): the current set and the one before
   alignas(16) float rs[N];               // e4m3: 2^e of a line's q
   float part[4][N];
-  alignas(16) float inv[N];
 };
 
-// D (+)= A B with e4m3 operands, 32 deep (split descriptors as umma_bf16_lo)
-__device__ __forceinline__ void tree_umma_f8(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}"
-      ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory");
+// Reduces v[col] over the lanes of a warp, 16 columns at once: lane i returns that of column i % 16.
+template <bool MAX>
+__device__ __forceinline__ float tree_reduce(float (&v)[16], int lane) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float got = __shfl_xor_sync(0xffffffffu, v[i], 16);
+    v[i] = MAX ? fmaxf(v[i], got) : v[i] + got;
+  }
+#pragma unroll
+  for (int s = 8; s >= 1; s >>= 1) {
+    const bool upper = (lane & s) != 0;
+#pragma unroll
+    for (int i = 0; i < s; ++i) {
+      const float send = upper ? v[i] : v[i + s], keep = upper ? v[i + s] : v[i];
+      const float got = __shfl_xor_sync(0xffffffffu, send, s);
+      v[i] = MAX ? fmaxf(keep, got) : keep + got;
+    }
+  }
+  return v[0];
 }
-// e4m3 x e4m3 -> fp32, both K-major
-__device__ __forceinline__ uint32_t tree_idesc_f8(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }
+
+// D (+)= A B: bf16 operands 16 deep, or e4m3 32 deep (split descriptors, as umma_bf16_lo; A and B with upper halves of their own)
+template <bool Q8>
+__device__ __forceinline__ void tree_umma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+  if (Q8)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %2};\n\tmov.b64 db, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 128 x n, fp32 sums; B with its rows (N) or with its columns (the depth) as the contiguous axis
+template <bool Q8>
+__device__ __forceinline__ uint32_t tree_idesc(int n, bool rows_contiguous) {
+  return (1u << 4) | (Q8 ? 0u : (1u << 7) | (1u << 10)) | (rows_contiguous ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+// Upper half of the descriptor of P: rows (keys) of `row` bytes = one swizzle span, 8 of them a group
+__device__ __forceinline__ uint32_t tree_p_desc_hi(int row) {
+  return (uint32_t)(8 * row >> 4) | (1u << 14) | ((row == 128 ? 2u : row == 64 ? 4u : 6u) << 29);
+}
 
 __device__ __forceinline__ uint32_t tree_e4m3x2(float x0, float x1) {
   return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ float2 tree_from_e4m3x2(uint32_t u) {
-  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)u, __NV_E4M3)));
+__device__ __forceinline__ __half2 tree_half2(uint32_t e4m3x2) {
+  return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)e4m3x2, __NV_E4M3));
+}
+__device__ __forceinline__ ptx::f32x2 tree_mul2(ptx::f32x2 a, ptx::f32x2 b) {
+  ptx::f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 // Queries of a CTA's lines into shared memory, rows of 128 bytes with the 128-byte swizzle; e4m3: hi, then lo.  VEC: 16-byte loads.
@@ -104,7 +151,7 @@ __device__ __forceinline__ void tree_queries(const TreeArgs& a, int b, int g, in
       for (int e = 0; e < 4; ++e) {
         const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
         const uint32_t h = tree_e4m3x2(x0, x1);
-        const float2 r = tree_from_e4m3x2(h);
+        const float2 r = __half22float2(tree_half2(h));
         hi[e >> 1] |= h << (16 * (e & 1));
         lo[e >> 1] |= tree_e4m3x2(x0 - r.x, x1 - r.y) << (16 * (e & 1));
       }
@@ -189,13 +236,13 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1);
       ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], N / 8); }
-    ptx::mbar_init(&c.p_full, N / 8 + 1);   // the softmax warps, and warp 3
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
+    ptx::mbar_init(&c.p_full, 4 * C::kGroups + 1);   // the softmax warps, and warp 3
     ptx::mbar_init(&c.p_empty, 1);
     ptx::fence_barrier_init();
   }
   if (threadIdx.x < 8) c.poison[threadIdx.x] = 0u;
-  if (threadIdx.x < N) c.m[0][threadIdx.x] = (int)threadIdx.x < n ? -INFINITY : INFINITY;   // (columns without a line: P = 0)
+  if (threadIdx.x < N) c.nm[0][threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
   if (warp == 1) {
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
@@ -236,8 +283,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   } else if (warp == 1 || warp == 2) {
     // ---------------- issuers of S^T = K Q^T (warp 1) and O^T (+)= V^T P^T (warp 2) ----------------
     const bool pv = warp == 2;
-    const uint32_t idesc = Q8 ? tree_idesc_f8(N) : ptx::idesc_bf16(128, N), hi32 = ptx::smem_desc_hi32();
+    const uint32_t idesc = tree_idesc<Q8>(N, pv), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
     const uint32_t b_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs)), ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
+    // from one product to the next: Q goes on in its row, P by the rows of 16 (32) keys; hi and lo lie behind one another
+    const uint32_t b_step = pv ? (uint32_t)((Q8 ? 32 : 16) * C::kPRow >> 4) : 2u, b_half = pv ? 4u * b_step : (uint32_t)(N * 128 >> 4);
     bool ok = true;
     for (int j = 0; j < T && ok; ++j) {
       const int s = j % C::kRing;
@@ -250,23 +299,22 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (ptx::elect_one()) {
         const uint32_t d = tmem_base + (pv ? (uint32_t)C::kColO : (uint32_t)(j & 1) * N);
         const uint32_t t = ring_lo + (uint32_t)s * (C::kSlot >> 4);
+        const int nk = pv ? (valid_keys(j) + (Q8 ? 31 : 15)) / (Q8 ? 32 : 16) : Q8 ? 4 : 8;
         if (Q8) {
-          const int nk = pv ? (valid_keys(j) + 31) >> 5 : 4;
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= nk) break;
-              tree_umma_f8(pv ? d + part * N : d, t + kk * 2, b_lo + part * (N * 128 >> 4) + kk * 2, hi32, idesc,
-                           (kk > 0 || (pv ? j > 0 : part > 0)) ? 1u : 0u);
+              tree_umma<Q8>(pv ? d + part * N : d, t + kk * 2, a_hi, b_lo + part * b_half + kk * b_step, b_hi, idesc,
+                            (kk > 0 || (pv ? j > 0 : part > 0)) ? 1u : 0u);
             }
         } else {
-          const int nk = pv ? attn_pv_keys(valid_keys(j)) >> 4 : 8;
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk) {
             if (kk >= nk) break;
-            const uint32_t k4 = (uint32_t)(kk & 3) * 2u, half = (uint32_t)(kk >> 2);
-            ptx::umma_bf16_lo(d, t + half * (kSub >> 4) + k4, b_lo + half * (N * 128 >> 4) + k4, hi32, idesc, (kk > 0 || (pv && j > 0)) ? 1u : 0u);
+            const uint32_t k4 = (uint32_t)(kk & 3), half = (uint32_t)(kk >> 2);
+            tree_umma<Q8>(d, t + half * (kSub >> 4) + k4 * 2u, a_hi, b_lo + half * b_half + k4 * b_step, b_hi, idesc, (kk > 0 || (pv && j > 0)) ? 1u : 0u);
           }
         }
         ptx::umma_commit(pv ? &c.v_empty[s] : &c.k_empty[s]);
@@ -296,9 +344,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (!__all_sync(0xffffffffu, ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag))) break;
     }
   } else {
-    // ---------------- softmax: one thread per key of the tile, 32 lines ----------------
-    const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * 32;
-    const int ng = min(32, n - col0);               // lines of this group (0 and less: none)
+    // ---------------- softmax: one thread per key of the tile, 16 lines ----------------
+    constexpr int CW = kTreeCols;
+    const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * CW;
+    const int ng = min(CW, n - col0);               // lines of this group (0 and less: none)
     const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
     const int bar = 1 + group;                      // named barrier of the group's four warps
     // who sees this thread's key, a bit for each line: tiles without drafted keys by the keys' number alone, the (at most
@@ -329,22 +378,18 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       k_scale = a.c.k_scale + at; v_scale = a.c.v_scale + at;
       if (key < valid_keys(0)) { ks = k_scale[0]; vs = v_scale[0]; }
     }
-    // this key's place in P (bf16: rows of 64 keys, two halves; e4m3: rows of 128), lines 8 i + e at 1024 i from that of line e
-    uint32_t p_addr[8];
+    // this key's row of P: 16-byte pieces of 16 (8) lines, exchanged by the swizzle of rows of 32, 64 or 128 bytes
+    const uint32_t p_row = ptx::smem_u32(Ps) + (uint32_t)(key * C::kPRow);
+    const int p_turn = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
+    auto p_piece = [&](int i) { return p_row + (uint32_t)(((group * (Q8 ? 1 : 2) + i) ^ p_turn) << 4); };
+    ptx::f32x2 acc[CW / 2];        // the lines' sums over this thread's keys
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t base = ptx::smem_u32(Ps) + (uint32_t)(col0 * 128 + e * 128);
-      p_addr[e] = Q8 ? base + (uint32_t)((((key >> 4) ^ e) << 4) + (key & 15))
-                     : base + (uint32_t)((key >> 6) * (N * 128) + ((((key & 63) >> 3) ^ e) << 4) + (key & 7) * 2);
-    }
-    float acc[32];   // the lines' sums over this thread's keys
-#pragma unroll
-    for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+    for (int i = 0; i < CW / 2; ++i) acc[i] = 0ull;
     int cur = 0;
     bool ok = true;
     for (int j = 0; j < T; ++j) {
       const int tile = tile0 + j, d = tile - draft0;
-      uint32_t sees = d < 0 ? 0xffffffffu : d == 0 ? seen[0] : d == 1 ? seen[1] : seen[2];
+      const uint32_t sees = d < 0 ? 0xffffffffu : d == 0 ? seen[0] : d == 1 ? seen[1] : seen[2];
       const float mul = Q8 ? ks * a.scale_log2 : a.scale_log2;
       // (a row of zeros may come with a scale of 0: it counts in the sum)
       const float v_sc = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;   // 2^-100
@@ -356,26 +401,29 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (!ok) break;
       ptx::tc_fence_after();
       const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
-      float v[32];
+      float v[CW];
       for (int turn = 0; turn < 2; ++turn) {
-        ptx::tmem_ld_32x32(s_col, v);
+        ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
         float most = -INFINITY;
         const float off = Q8 ? lv + 4.f : 0.f;
+        const ptx::f32x2 off2 = ptx::f2_pack(off, off), mul2 = ptx::f2_pack(mul, mul);
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
+        for (int e = 0; e < CW; e += 8) {
           if (e >= ng) break;
 #pragma unroll
           for (int i = e; i < e + 8; i += 4) {
-            const float4 m4 = *reinterpret_cast<const float4*>(&c.m[cur][col0 + i]);
+            const ulonglong2 nm = *reinterpret_cast<const ulonglong2*>(&c.nm[cur][col0 + i]);
+            ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
             if (Q8) {
-              const float4 r4 = *reinterpret_cast<const float4*>(&c.rs[col0 + i]);
-              v[i] *= r4.x; v[i + 1] *= r4.y; v[i + 2] *= r4.z; v[i + 3] *= r4.w;
+              const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col0 + i]);
+              s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
+              s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, nm.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, nm.y));
+            } else {
+              s0 = ptx::f2_fma(s0, mul2, nm.x); s1 = ptx::f2_fma(s1, mul2, nm.y);
             }
-            v[i] = fmaf(v[i], mul, off - m4.x);
-            v[i + 1] = fmaf(v[i + 1], mul, off - m4.y);
-            v[i + 2] = fmaf(v[i + 2], mul, off - m4.z);
-            v[i + 3] = fmaf(v[i + 3], mul, off - m4.w);
+            ptx::f2_unpack(s0, v[i], v[i + 1]);
+            ptx::f2_unpack(s1, v[i + 2], v[i + 3]);
           }
           if (sees != 0xffffffffu) {
 #pragma unroll
@@ -386,20 +434,21 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         }
         if (turn == 1 || ptx::all_agree(bar, 128, !(most > (Q8 ? kHeadE4m3 : kHeadBf16)))) break;
         // ---- the maxima move: from the scores themselves, over the group's four warps ----
-        ptx::tmem_ld_32x32(s_col, v);
+        ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < CW; ++i) {
           const float u = fmaf(Q8 ? v[i] * c.rs[col0 + i] : v[i], mul, lv);
           v[i] = i < ng && ((sees >> i) & 1u) ? u : -INFINITY;
         }
-        c.part[quarter][col0 + lane] = few_reduce<true>(v, lane);
+        const int col = col0 + (lane & 15);
+        const float part = tree_reduce<true>(v, lane);
+        if (lane < 16) c.part[quarter][col] = part;
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
-        const int col = col0 + lane;
-        const float old = c.m[cur][col];
+        const float old = -c.nm[cur][col];
         const float now = fmaxf(fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col])), old);
         const float f = old == -INFINITY ? 0.f : exp2f(old - now);
-        if (quarter == 0) c.m[cur ^ 1][col] = now;
+        if (quarter == 0 && lane < 16) c.nm[cur ^ 1][col] = -now;
         if (j > 0) {   // O^T: all products so far are in
           ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
         }
@@ -407,22 +456,20 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         cur ^= 1;
         if (!ok) break;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) acc[i] *= __shfl_sync(0xffffffffu, f, i);
+        for (int i = 0; i < CW / 2; ++i)
+          acc[i] = tree_mul2(acc[i], ptx::f2_pack(__shfl_sync(0xffffffffu, f, 2 * i), __shfl_sync(0xffffffffu, f, 2 * i + 1)));
         if (j > 0) {
           ptx::tc_fence_after();
 #pragma unroll
-          for (int part = 0; part < (Q8 ? 2 : 1); ++part)
+          for (int part_o = 0; part_o < (Q8 ? 2 : 1); ++part_o) {
+            const uint32_t at = t_lane + (uint32_t)(C::kColO + part_o * N);
+            ptx::tmem_ld_32x16(at, v);
+            ptx::tmem_ld_wait();
+            uint32_t w[16];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const uint32_t at = t_lane + (uint32_t)(C::kColO + part * N + half * 16);
-              float o[16];
-              ptx::tmem_ld_32x16(at, o);
-              ptx::tmem_ld_wait();
-              uint32_t w[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i] * __shfl_sync(0xffffffffu, f, half * 16 + i));
-              attn_tmem_st16(at, w);
-            }
+            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i] * __shfl_sync(0xffffffffu, f, i));
+            attn_tmem_st16(at, w);
+          }
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
@@ -431,77 +478,79 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.s_empty[j & 1]);
-      if (!Q8) {
+      uint32_t hi[8], lo[4];     // bf16: 16 lines; e4m3: 16 lines of each part
+      const ptx::f32x2 iv2 = ptx::f2_pack(iv, iv);
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          if (e >= ng) break;
+      for (int i = 0; i < 8; ++i) hi[i] = 0u;
 #pragma unroll
-          for (int i = e; i < e + 8; ++i) { v[i] = attn_ex2(v[i]); acc[i] += v[i]; }
-        }
-      } else {
+      for (int i = 0; i < 4; ++i) lo[i] = 0u;
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          if (e >= ng) break;
+      for (int e = 0; e < CW; e += 8) {
+        if (e >= ng) break;
 #pragma unroll
-          for (int i = e; i < e + 8; ++i) { v[i] = attn_ex2(v[i]); acc[i] = fmaf(v[i], iv, acc[i]); }
+        for (int i = e; i < e + 8; i += 2) {
+          const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]);
+          const ptx::f32x2 p = ptx::f2_pack(p0, p1);
+          if (!Q8) {
+            acc[i / 2] = ptx::f2_add(acc[i / 2], p);
+            const __nv_bfloat162 w = __floats2bfloat162_rn(p0, p1);
+            hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w);
+          } else {
+            acc[i / 2] = ptx::f2_fma(p, iv2, acc[i / 2]);
+            // hi: the value (of 11 bits) rounded to 4; lo: 16 times the rest
+            const __half2 ph = __floats2half2_rn(p0, p1);
+            const uint32_t h = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&ph), __NV_SATFINITE, __NV_E4M3);
+            const __half2 rest = __hfma2(tree_half2(h), __float2half2_rn(-16.f), __hmul2(ph, __float2half2_rn(16.f)));
+            const uint32_t l = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&rest), __NV_SATFINITE, __NV_E4M3);
+            if (i & 2) { hi[i / 4] = __byte_perm(hi[i / 4], h, 0x5410); lo[i / 4] = __byte_perm(lo[i / 4], l, 0x5410); }
+            else { hi[i / 4] = h; lo[i / 4] = l; }
+          }
         }
       }
       // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
       if (j > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
       if (!ok) continue;
-#pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        if (e >= ng) break;
-        if (!Q8) {
-#pragma unroll
-          for (int i = e; i < e + 8; ++i)
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_addr[i & 7] + (uint32_t)(i >> 3) * 1024u),
-                         "h"(__bfloat16_as_ushort(__float2bfloat16_rn(v[i]))) : "memory");
-        } else {
-#pragma unroll
-          for (int i = e; i < e + 8; i += 2) {
-            // hi: the value rounded, lo: 16 times the rest
-            const uint32_t hi = tree_e4m3x2(v[i], v[i + 1]);
-            const float2 r = tree_from_e4m3x2(hi);
-            const uint32_t lo = tree_e4m3x2((v[i] - r.x) * 16.f, (v[i + 1] - r.y) * 16.f);
-            const uint32_t a0 = p_addr[i & 7] + (uint32_t)(i >> 3) * 1024u, a1 = p_addr[(i + 1) & 7] + (uint32_t)(i >> 3) * 1024u;
-            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a0), "r"(hi) : "memory");
-            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a1), "r"(hi >> 8) : "memory");
-            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a0 + N * 128), "r"(lo) : "memory");
-            asm volatile("st.shared.b8 [%0], %1;" ::"r"(a1 + N * 128), "r"(lo >> 8) : "memory");
-          }
-        }
-      }
+      auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+      };
+      st16(p_piece(0), hi[0], hi[1], hi[2], hi[3]);
+      if (Q8) st16(p_piece(0) + 128 * C::kPRow, lo[0], lo[1], lo[2], lo[3]);
+      else st16(p_piece(1), hi[4], hi[5], hi[6], hi[7]);
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.p_full);
     }
     // O^T is complete once the last P has been read
     if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag));
-    c.part[quarter][col0 + lane] = few_reduce<false>(acc, lane);
-    if (quarter == 0) c.inv[col0 + lane] = c.m[cur][col0 + lane];     // (for the output below)
+    float sum[CW];
+#pragma unroll
+    for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
+    const float part = tree_reduce<false>(sum, lane);
+    if (lane < 16) {
+      c.part[quarter][col0 + lane] = part;
+      if (quarter == 0) c.rs[col0 + lane] = -c.nm[cur][col0 + lane];     // (for the output below)
+    }
   }
   // ---------------- output ----------------
   __syncthreads();
   const bool failed = c.abort_flag != 0, alone = tree_stretches(a, b) == 1;
   if (warp >= 4) {
-    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * 32, ng = min(32, n - col0);
+    constexpr int CW = kTreeCols;
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * CW, ng = min(CW, n - col0);
     if (ng > 0) {
-      float o[32];
+      float o[CW];
       if (!failed) {
         const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
         ptx::tc_fence_after();
-        ptx::tmem_ld_32x32(at, o);
-        ptx::tmem_ld_wait();
+        ptx::tmem_ld_32x16(at, o);
         if (Q8) {
+          float lo[CW];
+          ptx::tmem_ld_32x16(at + (uint32_t)N, lo);
+          ptx::tmem_ld_wait();
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float lo[16];
-            ptx::tmem_ld_32x16(at + (uint32_t)(N + half * 16), lo);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[half * 16 + i] = fmaf(lo[i], 1.f / 16.f, o[half * 16 + i]) * (1.f / 16.f);
-          }
+          for (int i = 0; i < CW; ++i) o[i] = fmaf(lo[i], 1.f / 16.f, o[i]) * (1.f / 16.f);
+        } else {
+          ptx::tmem_ld_wait();
         }
       }
       // lane = line: its sum, whether it sees a key that is not finite, its place
@@ -515,12 +564,12 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
             if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
         if (bad) l = __uint_as_float(0x7fffffffu);
         if (!alone && quarter == 0)
-          a.part_ml[(size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)] = make_float2(c.inv[col], l);
+          a.part_ml[(size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)] = make_float2(c.rs[col], l);
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
       int r = (line0 + col0) / G, i_in = (line0 + col0) % G;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
+      for (int i = 0; i < CW; ++i) {
         if (i >= ng) break;
         const float w = __shfl_sync(0xffffffffu, inv, i);
         const int h = g * G + i_in, dim = quarter * 32 + lane;
