@@ -22,9 +22,10 @@
 // P lies in shared memory as the threads have it, a row of N values for a key (the product takes it with the lines as the
 // contiguous axis): a thread stores 16 bytes at a time, where rows of keys would take a store for every value.
 //
-// Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, 3 = puts V^T tiles in order
+// Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
-// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every kTreeCols lines.
+// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every kTreeCols lines (warp 3
+// has nothing to do: a warp reads the quarter of TMEM's lanes that its number says).
 #pragma once
 #include "tc_attn_parts.cuh"
 #include "tree_attn.cuh"
@@ -32,16 +33,20 @@
 namespace dc {
 
 constexpr int kTreeCols = 16;    // lines of a softmax warp
+#ifndef RK
+#define RK 2
+#define RV 2
+#endif
 
 template <int N, bool Q8>
 struct TreeTc {
   static constexpr int kGroups = N / kTreeCols, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
-  static constexpr int kRing = Q8 ? (N == 32 ? 2 : 4) : 3;     // slots of each ring
+  static constexpr int kRingK = Q8 ? (N == 32 ? RK : 4) : 3, kRingV = Q8 ? (N == 32 ? RV : 4) : 3;     // slots of the rings
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
   static constexpr int kCtl = 3072;
-  static constexpr int kSmem = 2 * kOperand + 2 * kRing * kSlot + kCtl;
+  static constexpr int kSmem = 2 * kOperand + (kRingK + kRingV) * kSlot + kCtl;
   static constexpr int kPRow = Q8 ? N : 2 * N;                  // bytes of a key's row of P (of its hi or lo part): 32, 64 or 128
   static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : 256;   // TMEM: S^T twice, O^T (its two parts)
 };
@@ -109,6 +114,21 @@ __device__ __forceinline__ uint32_t tree_p_desc_hi(int row) {
 
 __device__ __forceinline__ uint32_t tree_e4m3x2(float x0, float x1) {
   return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
+}
+// Four values, two in an f16x2, as hi + lo / 16 of e4m3: hi rounded, lo of 16 times the rest
+__device__ __forceinline__ void tree_split4(__half2 x, __half2 y, uint32_t& hi, uint32_t& lo) {
+  const __half2 m16 = __float2half2_rn(-16.f);
+  const __half2 x16 = __hmul2(x, __float2half2_rn(16.f)), y16 = __hmul2(y, __float2half2_rn(16.f));
+  asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 r0, r1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 h0, %2;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h1, %3;\n\t"
+      "mov.b32 %0, {h0, h1};\n\t"
+      "cvt.rn.f16x2.e4m3x2 r0, h0;\n\tcvt.rn.f16x2.e4m3x2 r1, h1;\n\t"
+      "fma.rn.f16x2 r0, r0, %4, %5;\n\tfma.rn.f16x2 r1, r1, %4, %6;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 l0, r0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l1, r1;\n\t"
+      "mov.b32 %1, {l0, l1};\n\t}"
+      : "=r"(hi), "=r"(lo)
+      : "r"(*reinterpret_cast<const uint32_t*>(&x)), "r"(*reinterpret_cast<const uint32_t*>(&y)), "r"(*reinterpret_cast<const uint32_t*>(&m16)),
+        "r"(*reinterpret_cast<const uint32_t*>(&x16)), "r"(*reinterpret_cast<const uint32_t*>(&y16)));
 }
 __device__ __forceinline__ __half2 tree_half2(uint32_t e4m3x2) {
   return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)e4m3x2, __NV_E4M3));
@@ -221,8 +241,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
   if (n <= 0 || T <= 0) return;
-  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRing * C::kSlot;
-  TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRing * C::kSlot);
+  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRingK * C::kSlot;
+  TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if ((ptx::smem_u32(smem_tree) & 1023u) != 0) {   // (it is all the shared memory there is and starts on such a boundary)
@@ -232,12 +252,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
 
   if (threadIdx.x == 0) {
     c.abort_flag = 0; c.late_flag = 0;
-    for (int i = 0; i < C::kRing; ++i) {
-      ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1);
-      ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1);
-    }
+    for (int i = 0; i < C::kRingK; ++i) { ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1); }
+    for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
-    ptx::mbar_init(&c.p_full, 4 * C::kGroups + 1);   // the softmax warps, and warp 3
+    ptx::mbar_init(&c.p_full, 4 * C::kGroups);       // the softmax warps
     ptx::mbar_init(&c.p_empty, 1);
     ptx::fence_barrier_init();
   }
@@ -259,20 +277,24 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   int* abort_flag = &c.abort_flag;
   int loads = 0;   // of the producer thread: tiles of K and of V^T, in turn
   auto valid_keys = [&](int j) { return min(kTreeTile, keys - (tile0 + j) * kTreeTile); };
+  // V^T tiles that are put in order before their product: the stretch's last ones
+  auto drafted = [&](int j) { return a.mask && (tile0 + j) * kTreeTile + valid_keys(j) > ctx; };
+  auto ragged = [&](int j) { return (valid_keys(j) & (Q8 ? 31 : 15)) != 0; };
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer ----------------
       const int krow = (b * nkv + g) * a.c.max_ctx, vrow = (b * nkv + g) * kHd;
       for (int j = 0; j < T; ++j) {
-        const int s = j % C::kRing, key = (tile0 + j) * kTreeTile;
-        const uint32_t ph = (uint32_t)(j / C::kRing) & 1u;
-        if (!ptx::mbar_wait(&c.k_empty[s], ph ^ 1u, abort_flag)) break;
+        int s = j % C::kRingK;
+        const int key = (tile0 + j) * kTreeTile;
+        if (!ptx::mbar_wait(&c.k_empty[s], ((uint32_t)(j / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
         uint8_t* dst = kring + (size_t)s * C::kSlot;
         ptx::mbar_expect_tx(&c.k_full[s], C::kSlot);
         ptx::tma_load_2d(dst, &map_k, &c.k_full[s], 0, krow + key);
         if (!Q8) ptx::tma_load_2d(dst + kSub, &map_k, &c.k_full[s], 64, krow + key);
         ++loads;
-        if (!ptx::mbar_wait(&c.v_empty[s], ph ^ 1u, abort_flag)) break;
+        s = j % C::kRingV;
+        if (!ptx::mbar_wait(&c.v_empty[s], ((uint32_t)(j / C::kRingV) & 1u) ^ 1u, abort_flag)) break;
         dst = vring + (size_t)s * C::kSlot;
         ptx::mbar_expect_tx(&c.v_full[s], C::kSlot);
         ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
@@ -289,10 +311,27 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     const uint32_t b_step = pv ? (uint32_t)((Q8 ? 32 : 16) * C::kPRow >> 4) : 2u, b_half = pv ? 4u * b_step : (uint32_t)(N * 128 >> 4);
     bool ok = true;
     for (int j = 0; j < T && ok; ++j) {
-      const int s = j % C::kRing;
-      if (pv) ok = ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
-      else if (j >= 2) ok = ptx::mbar_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
-      ok = ok && ptx::mbar_wait(pv ? &c.v_full[s] : &c.k_full[s], (uint32_t)(j / C::kRing) & 1u, abort_flag);
+      const int s = pv ? j % C::kRingV : j % C::kRingK;
+      if (pv) {
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.v_full[s], (uint32_t)(j / C::kRingV) & 1u, abort_flag));
+        if (!ok) break;
+        if (drafted(j) || ragged(j)) {     // (while the softmax warps make P)
+          const int key0 = (tile0 + j) * kTreeTile, valid = valid_keys(j);
+          uint8_t* tile = vring + (size_t)s * C::kSlot;
+          if (ragged(j))
+            for (int rr = lane; rr < 128; rr += 32) {
+              if (Q8) tree_clear_v8(tile, rr, valid);
+              else attn_clear_v(tile, rr, valid);
+            }
+          if (drafted(j)) tree_clean_v<Q8>(tile, max(0, ctx - key0), valid, max(0, key0 - ctx), c.poison);
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+        }
+        ok = ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
+      } else {
+        if (j >= 2) ok = ptx::mbar_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
+        ok = ok && ptx::mbar_wait(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
+      }
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       ptx::tc_fence_after();
@@ -322,28 +361,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       }
       __syncwarp();
     }
-  } else if (warp == 3) {
-    // ---------------- V^T tiles: beyond the valid keys, and drafted values that are not finite ----------------
-    for (int j = 0; j < T; ++j) {
-      const int s = j % C::kRing, key0 = (tile0 + j) * kTreeTile, valid = valid_keys(j);
-      const bool ragged = (valid & (Q8 ? 31 : 15)) != 0, drafted = a.mask && key0 + valid > ctx;
-      if (ragged || drafted) {
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(&c.v_full[s], (uint32_t)(j / C::kRing) & 1u, abort_flag))) break;
-        uint8_t* tile = vring + (size_t)s * C::kSlot;
-        if (ragged)
-          for (int rr = lane; rr < 128; rr += 32) {
-            if (Q8) tree_clear_v8(tile, rr, valid);
-            else attn_clear_v(tile, rr, valid);
-          }
-        if (drafted) tree_clean_v<Q8>(tile, max(0, ctx - key0), valid, max(0, key0 - ctx), c.poison);
-        ptx::fence_proxy_async_smem();
-        __syncwarp();
-      }
-      if (lane == 0) ptx::mbar_arrive(&c.p_full);
-      // (not ahead of the tile: its next arrival belongs to the next phase)
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag))) break;
-    }
-  } else {
+  } else if (warp >= 4) {
     // ---------------- softmax: one thread per key of the tile, 16 lines ----------------
     constexpr int CW = kTreeCols;
     const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * CW;
@@ -385,6 +403,32 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     ptx::f32x2 acc[CW / 2];        // the lines' sums over this thread's keys
 #pragma unroll
     for (int i = 0; i < CW / 2; ++i) acc[i] = 0ull;
+    // the exponents of P from the scores, -infinity where a line does not see the key
+    auto exponents = [&](float (&v)[CW], const float* nm, float mul, float lv, uint32_t sees) {
+      const ptx::f32x2 off2 = ptx::f2_pack(lv + 4.f, lv + 4.f), mul2 = ptx::f2_pack(mul, mul);
+#pragma unroll
+      for (int e = 0; e < CW; e += 8) {
+        if (e >= ng) break;
+#pragma unroll
+        for (int i = e; i < e + 8; i += 4) {
+          const ulonglong2 m2 = *reinterpret_cast<const ulonglong2*>(nm + col0 + i);
+          ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
+          if (Q8) {
+            const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col0 + i]);
+            s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
+            s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, m2.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, m2.y));
+          } else {
+            s0 = ptx::f2_fma(s0, mul2, m2.x); s1 = ptx::f2_fma(s1, mul2, m2.y);
+          }
+          ptx::f2_unpack(s0, v[i], v[i + 1]);
+          ptx::f2_unpack(s1, v[i + 2], v[i + 3]);
+        }
+        if (sees != 0xffffffffu) {
+#pragma unroll
+          for (int i = e; i < e + 8; ++i) v[i] = (sees >> i) & 1u ? v[i] : -INFINITY;
+        }
+      }
+    };
     int cur = 0;
     bool ok = true;
     for (int j = 0; j < T; ++j) {
@@ -396,43 +440,22 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       const float lv = Q8 ? __log2f(v_sc) : 0.f, iv = Q8 && v_sc <= 3.402823466e38f ? __frcp_rn(v_sc * 16.f) : 0.f;
       if (Q8 && j + 1 < T && key < valid_keys(j + 1)) { ks = k_scale[(size_t)(j + 1) * kTreeTile]; vs = v_scale[(size_t)(j + 1) * kTreeTile]; }
       ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag));
-      // (whatever their waits said, the four warps of a group come to its barriers together)
-      ok = ptx::all_agree(bar, 128, ok);
-      if (!ok) break;
+      // (whatever their waits said, the four warps of a group come to its barriers together: a wait that ran out is a no in the
+      // vote on the maxima, and the vote behind it ends the loop for all four)
       ptx::tc_fence_after();
       const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
       float v[CW];
-      for (int turn = 0; turn < 2; ++turn) {
-        ptx::tmem_ld_32x16(s_col, v);
-        ptx::tmem_ld_wait();
-        float most = -INFINITY;
-        const float off = Q8 ? lv + 4.f : 0.f;
-        const ptx::f32x2 off2 = ptx::f2_pack(off, off), mul2 = ptx::f2_pack(mul, mul);
+      ptx::tmem_ld_32x16(s_col, v);
+      ptx::tmem_ld_wait();
+      exponents(v, c.nm[cur], mul, lv, sees);
+      float most = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < CW; e += 8) {
-          if (e >= ng) break;
+      for (int i = 0; i < CW; i += 8) {
+        if (i >= ng) break;
 #pragma unroll
-          for (int i = e; i < e + 8; i += 4) {
-            const ulonglong2 nm = *reinterpret_cast<const ulonglong2*>(&c.nm[cur][col0 + i]);
-            ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
-            if (Q8) {
-              const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col0 + i]);
-              s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
-              s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, nm.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, nm.y));
-            } else {
-              s0 = ptx::f2_fma(s0, mul2, nm.x); s1 = ptx::f2_fma(s1, mul2, nm.y);
-            }
-            ptx::f2_unpack(s0, v[i], v[i + 1]);
-            ptx::f2_unpack(s1, v[i + 2], v[i + 3]);
-          }
-          if (sees != 0xffffffffu) {
-#pragma unroll
-            for (int i = e; i < e + 8; ++i) v[i] = (sees >> i) & 1u ? v[i] : -INFINITY;
-          }
-#pragma unroll
-          for (int i = e; i < e + 8; i += 2) most = ptx::fmax3(most, v[i], v[i + 1]);
-        }
-        if (turn == 1 || ptx::all_agree(bar, 128, !(most > (Q8 ? kHeadE4m3 : kHeadBf16)))) break;
+        for (int e = i; e < i + 8; e += 2) most = ptx::fmax3(most, v[e], v[e + 1]);
+      }
+      if (!ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)))) {
         // ---- the maxima move: from the scores themselves, over the group's four warps ----
         ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
@@ -450,7 +473,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         const float f = old == -INFINITY ? 0.f : exp2f(old - now);
         if (quarter == 0 && lane < 16) c.nm[cur ^ 1][col] = -now;
         if (j > 0) {   // O^T: all products so far are in
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+          ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
         }
         ok = ptx::all_agree(bar, 128, ok);
         cur ^= 1;
@@ -473,6 +496,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
+        ptx::tmem_ld_32x16(s_col, v);
+        ptx::tmem_ld_wait();
+        exponents(v, c.nm[cur], mul, lv, sees);
       }
       if (!ok) break;
       ptx::tc_fence_before();
@@ -488,22 +514,18 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       for (int e = 0; e < CW; e += 8) {
         if (e >= ng) break;
 #pragma unroll
-        for (int i = e; i < e + 8; i += 2) {
-          const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]);
-          const ptx::f32x2 p = ptx::f2_pack(p0, p1);
+        for (int i = e; i < e + 8; i += 4) {
+          const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]), p2 = attn_ex2(v[i + 2]), p3 = attn_ex2(v[i + 3]);
           if (!Q8) {
-            acc[i / 2] = ptx::f2_add(acc[i / 2], p);
-            const __nv_bfloat162 w = __floats2bfloat162_rn(p0, p1);
-            hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w);
+            acc[i / 2] = ptx::f2_add(acc[i / 2], ptx::f2_pack(p0, p1));
+            acc[i / 2 + 1] = ptx::f2_add(acc[i / 2 + 1], ptx::f2_pack(p2, p3));
+            const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
+            hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
+            hi[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
           } else {
-            acc[i / 2] = ptx::f2_fma(p, iv2, acc[i / 2]);
-            // hi: the value (of 11 bits) rounded to 4; lo: 16 times the rest
-            const __half2 ph = __floats2half2_rn(p0, p1);
-            const uint32_t h = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&ph), __NV_SATFINITE, __NV_E4M3);
-            const __half2 rest = __hfma2(tree_half2(h), __float2half2_rn(-16.f), __hmul2(ph, __float2half2_rn(16.f)));
-            const uint32_t l = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&rest), __NV_SATFINITE, __NV_E4M3);
-            if (i & 2) { hi[i / 4] = __byte_perm(hi[i / 4], h, 0x5410); lo[i / 4] = __byte_perm(lo[i / 4], l, 0x5410); }
-            else { hi[i / 4] = h; lo[i / 4] = l; }
+            acc[i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[i / 2]);
+            acc[i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[i / 2 + 1]);
+            tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[i / 4], lo[i / 4]);
           }
         }
       }
@@ -583,10 +605,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   }
   if (loads > 0 && c.abort_flag != 0) {
     // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)
-    for (int it = max(0, loads - 2 * C::kRing); it < loads; ++it) {
-      const int j = it >> 1;
-      ptx::mbar_wait((it & 1) == 0 ? &c.k_full[j % C::kRing] : &c.v_full[j % C::kRing], (uint32_t)(j / C::kRing) & 1u, &c.late_flag);
-    }
+    for (int j = max(0, (loads + 1) / 2 - C::kRingK); j < (loads + 1) / 2; ++j)
+      ptx::mbar_wait(&c.k_full[j % C::kRingK], (uint32_t)(j / C::kRingK) & 1u, &c.late_flag);
+    for (int j = max(0, loads / 2 - C::kRingV); j < loads / 2; ++j)
+      ptx::mbar_wait(&c.v_full[j % C::kRingV], (uint32_t)(j / C::kRingV) & 1u, &c.late_flag);
   }
   ptx::tc_fence_before();
   __syncthreads();
