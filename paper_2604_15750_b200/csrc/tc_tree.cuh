@@ -139,6 +139,46 @@ __device__ __forceinline__ ptx::f32x2 tree_mul2(ptx::f32x2 a, ptx::f32x2 b) {
   return r;
 }
 
+// A bounded wait as ptx::mbar_wait, without the hint that lets a try sleep: the warps here wait little, and a try with the
+// hint is a loop of its own, whose instructions the softmax warps of the other CTA on the SM would have to share with.
+__device__ __forceinline__ bool tree_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred P;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 P, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, P;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __noinline__ bool tree_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  const unsigned long long t0 = ptx::globaltimer();
+  uint32_t polls = 0;
+  while (!tree_try(bar, parity)) {
+    if ((++polls & 0xff) == 0) {
+      if (*abort_flag) return false;
+      if (ptx::globaltimer() - t0 > ptx::g_wait_limit_ns) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  const uint32_t at = ptx::smem_u32(bar);
+  return tree_try(at, parity) || tree_wait_on(at, parity, abort_flag);
+}
+__device__ __forceinline__ float tree_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float tree_lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Queries of a CTA's lines into shared memory, rows of 128 bytes with the 128-byte swizzle; e4m3: hi, then lo.  VEC: 16-byte loads.
 template <int N, bool Q8, bool VEC>
 __device__ __forceinline__ void tree_queries(const TreeArgs& a, int b, int g, int line0, int n, uint8_t* Qs, float* rs) {
@@ -287,14 +327,14 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       for (int j = 0; j < T; ++j) {
         int s = j % C::kRingK;
         const int key = (tile0 + j) * kTreeTile;
-        if (!ptx::mbar_wait(&c.k_empty[s], ((uint32_t)(j / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
+        if (!tree_wait(&c.k_empty[s], ((uint32_t)(j / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
         uint8_t* dst = kring + (size_t)s * C::kSlot;
         ptx::mbar_expect_tx(&c.k_full[s], C::kSlot);
         ptx::tma_load_2d(dst, &map_k, &c.k_full[s], 0, krow + key);
         if (!Q8) ptx::tma_load_2d(dst + kSub, &map_k, &c.k_full[s], 64, krow + key);
         ++loads;
         s = j % C::kRingV;
-        if (!ptx::mbar_wait(&c.v_empty[s], ((uint32_t)(j / C::kRingV) & 1u) ^ 1u, abort_flag)) break;
+        if (!tree_wait(&c.v_empty[s], ((uint32_t)(j / C::kRingV) & 1u) ^ 1u, abort_flag)) break;
         dst = vring + (size_t)s * C::kSlot;
         ptx::mbar_expect_tx(&c.v_full[s], C::kSlot);
         ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
@@ -313,7 +353,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int j = 0; j < T && ok; ++j) {
       const int s = pv ? j % C::kRingV : j % C::kRingK;
       if (pv) {
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.v_full[s], (uint32_t)(j / C::kRingV) & 1u, abort_flag));
+        ok = __all_sync(0xffffffffu, tree_wait(&c.v_full[s], (uint32_t)(j / C::kRingV) & 1u, abort_flag));
         if (!ok) break;
         if (drafted(j) || ragged(j)) {     // (while the softmax warps make P)
           const int key0 = (tile0 + j) * kTreeTile, valid = valid_keys(j);
@@ -327,10 +367,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           ptx::fence_proxy_async_smem();
           __syncwarp();
         }
-        ok = ptx::mbar_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
+        ok = tree_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
       } else {
-        if (j >= 2) ok = ptx::mbar_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
-        ok = ok && ptx::mbar_wait(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
+        if (j >= 2) ok = tree_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
+        ok = ok && tree_wait(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
       }
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
@@ -437,9 +477,12 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       const float mul = Q8 ? ks * a.scale_log2 : a.scale_log2;
       // (a row of zeros may come with a scale of 0: it counts in the sum)
       const float v_sc = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;   // 2^-100
-      const float lv = Q8 ? __log2f(v_sc) : 0.f, iv = Q8 && v_sc <= 3.402823466e38f ? __frcp_rn(v_sc * 16.f) : 0.f;
-      if (Q8 && j + 1 < T && key < valid_keys(j + 1)) { ks = k_scale[(size_t)(j + 1) * kTreeTile]; vs = v_scale[(size_t)(j + 1) * kTreeTile]; }
-      ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag));
+      const float lv = Q8 ? tree_lg2(v_sc) : 0.f, iv = Q8 && v_sc <= 3.402823466e38f ? tree_rcp(v_sc * 16.f) : 0.f;
+      if (Q8) {
+        k_scale += kTreeTile; v_scale += kTreeTile;
+        if (j + 1 < T && key < valid_keys(j + 1)) { ks = *k_scale; vs = *v_scale; }
+      }
+      ok = ok && __all_sync(0xffffffffu, tree_wait(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag));
       // (whatever their waits said, the four warps of a group come to its barriers together: a wait that ran out is a no in the
       // vote on the maxima, and the vote behind it ends the loop for all four)
       ptx::tc_fence_after();
@@ -473,7 +516,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         const float f = old == -INFINITY ? 0.f : exp2f(old - now);
         if (quarter == 0 && lane < 16) c.nm[cur ^ 1][col] = -now;
         if (j > 0) {   // O^T: all products so far are in
-          ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+          ok = ok && __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
         }
         ok = ptx::all_agree(bar, 128, ok);
         cur ^= 1;
@@ -530,7 +573,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         }
       }
       // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
-      if (j > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+      if (j > 0) ok = __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
       if (!ok) continue;
       auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -543,7 +586,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (lane == 0) ptx::mbar_arrive(&c.p_full);
     }
     // O^T is complete once the last P has been read
-    if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag));
+    if (ok) ok = __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag));
     float sum[CW];
 #pragma unroll
     for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
@@ -606,9 +649,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   if (loads > 0 && c.abort_flag != 0) {
     // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)
     for (int j = max(0, (loads + 1) / 2 - C::kRingK); j < (loads + 1) / 2; ++j)
-      ptx::mbar_wait(&c.k_full[j % C::kRingK], (uint32_t)(j / C::kRingK) & 1u, &c.late_flag);
+      tree_wait(&c.k_full[j % C::kRingK], (uint32_t)(j / C::kRingK) & 1u, &c.late_flag);
     for (int j = max(0, loads / 2 - C::kRingV); j < loads / 2; ++j)
-      ptx::mbar_wait(&c.v_full[j % C::kRingV], (uint32_t)(j / C::kRingV) & 1u, &c.late_flag);
+      tree_wait(&c.v_full[j % C::kRingV], (uint32_t)(j / C::kRingV) & 1u, &c.late_flag);
   }
   ptx::tc_fence_before();
   __syncthreads();
