@@ -12,11 +12,11 @@
 // e4m3 too, and one e4m3 number has 4 significant bits, so it is given as the sum of two:
 //   q = 2^e (hi + lo): 4 + 4 bits hold the 8 of a bf16 value exactly (per line, largest magnitude in [128, 256); what is
 //     2^10 below that is off by 2^-18 of it at most); both products go to the same accumulator
-//   P' = 2^(t + log2 v_scale + 4 - m) = hi + lo / 16: 8 bits, not finer than 2^-14 where the largest is 16 .. 256; two accumulators
+//   P' = 2^(t + log2 v_scale + 4 - m) = hi + lo / 16: 8 bits, not finer than 2^-14 where the largest is 8 .. 446; two accumulators
 // The scales are factors of a key, and a thread has one key: K's goes into t, V's into P', so that the sum of a line
 // takes P' / (16 v_scale).  The maximum m is that of t + log2 v_scale.
 //
-// m of a line is the maximum of the first tile that it sees and moves only when a later tile has a t above it by more than kHead
+// m of a line is about the maximum of the first tile that it sees and moves only when a later tile has a t far above it
 // (a vote of the four warps that hold a line's keys): then O and the sums are scaled by 2^(m_old - m_new).
 //
 // P lies in shared memory as the threads have it, a row of N values for a key (the product takes it with the lines as the
@@ -35,7 +35,7 @@ namespace dc {
 constexpr int kTreeCols = 16;    // lines of a softmax warp
 #ifndef RK
 #define RK 2
-#define RV 2
+#define RV 3
 #endif
 
 template <int N, bool Q8>
@@ -50,38 +50,41 @@ struct TreeTc {
   static constexpr int kPRow = Q8 ? N : 2 * N;                  // bytes of a key's row of P (of its hi or lo part): 32, 64 or 128
   static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : 256;   // TMEM: S^T twice, O^T (its two parts)
 };
-constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.f;   // (P' = 2^(4 + 4) at most: e4m3 ends at 448)
+// P' of e4m3 is 2^8.8 at most (e4m3 ends at 448): m is set 1 above the maximum, which leaves 5.8 for later tiles, and each time that
+// m moves costs about half a tile.
+constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.8f, kAhead = 1.f;
 
 template <int N>
 struct TreeCtl {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full, p_empty;
   uint32_t tmem_base;
-  int abort_flag, late_flag;
+  int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
   alignas(16) float nm[2][N];            // the lines' maxima, negative (log2 units): the current set and the one before
   alignas(16) float rs[N];               // e4m3: 2^e of a line's q
   float part[4][N];
 };
 
-// Reduces v[col] over the lanes of a warp, 16 columns at once: lane i returns that of column i % 16.
-template <bool MAX>
-__device__ __forceinline__ float tree_reduce(float (&v)[16], int lane) {
+// Sum of v[col] over the lanes of a warp, 16 columns at once: lane i returns that of column i % 16.
+__device__ __forceinline__ float tree_sum(float (&v)[16], int lane) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float got = __shfl_xor_sync(0xffffffffu, v[i], 16);
-    v[i] = MAX ? fmaxf(v[i], got) : v[i] + got;
-  }
+  for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
 #pragma unroll
   for (int s = 8; s >= 1; s >>= 1) {
     const bool upper = (lane & s) != 0;
 #pragma unroll
     for (int i = 0; i < s; ++i) {
       const float send = upper ? v[i] : v[i + s], keep = upper ? v[i + s] : v[i];
-      const float got = __shfl_xor_sync(0xffffffffu, send, s);
-      v[i] = MAX ? fmaxf(keep, got) : keep + got;
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, s);
     }
   }
   return v[0];
+}
+// largest value of a warp, NaN passed over
+__device__ __forceinline__ float tree_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // D (+)= A B: bf16 operands 16 deep, or e4m3 32 deep (split descriptors, as umma_bf16_lo; A and B with upper halves of their own)
@@ -179,47 +182,50 @@ __device__ __forceinline__ float tree_lg2(float x) {
   return y;
 }
 
-// Queries of a CTA's lines into shared memory, rows of 128 bytes with the 128-byte swizzle; e4m3: hi, then lo.  VEC: 16-byte loads.
-template <int N, bool Q8, bool VEC>
-__device__ __forceinline__ void tree_queries(const TreeArgs& a, int b, int g, int line0, int n, uint8_t* Qs, float* rs) {
-  for (int i = threadIdx.x; i < N * 16; i += TreeTc<N, Q8>::kThreads) {   // (N * 16 and the threads are whole warps)
-    const int line = i >> 4, c = i & 15, m = line0 + line;      // 8 dims of a line
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (line < n) {
-      const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + b * a.qs[0] + (m / a.group) * a.qs[1] + (g * a.group + m % a.group) * a.qs[2] + c * 8;
-      if (VEC) {
-        const uint4 v = *reinterpret_cast<const uint4*>(q);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (uint32_t)__bfloat16_as_ushort(q[2 * e]) | (uint32_t)__bfloat16_as_ushort(q[2 * e + 1]) << 16;
-      }
-    }
-    if (!Q8) {
-      *reinterpret_cast<uint4*>(Qs + (c >> 3) * (N * 128) + line * 128 + (((c & 7) ^ (line & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-      uint32_t top = 0;     // magnitudes order as their patterns do
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
-#pragma unroll
-      for (int s = 8; s >= 1; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const int ex = max((int)(top >> 7), 20) - 127;            // of the largest magnitude
-      const float f = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
-      if (c == 0) rs[line] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)(127 - 7 + ex) << 23);
-      uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
-        const uint32_t h = tree_e4m3x2(x0, x1);
-        const float2 r = __half22float2(tree_half2(h));
-        hi[e >> 1] |= h << (16 * (e & 1));
-        lo[e >> 1] |= tree_e4m3x2(x0 - r.x, x1 - r.y) << (16 * (e & 1));
-      }
-      uint8_t* at = Qs + line * 128 + (((c >> 1) ^ (line & 7)) << 4) + (c & 1) * 8;
-      *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(at + N * 128) = make_uint2(lo[0], lo[1]);
-    }
+// Queries of a CTA's lines, 8 dims of a line each, up to two a thread: the loads, and what becomes of them in shared memory (rows of
+// 128 bytes with the 128-byte swizzle; e4m3: hi, then lo).
+template <int N, bool Q8>
+__device__ __forceinline__ void tree_load_q(const TreeArgs& a, int b, int g, int line0, int n, int vec, int item, uint4& w) {
+  const int line = item >> 4, c = item & 15;
+  w = make_uint4(0u, 0u, 0u, 0u);
+  if (line >= n) return;
+  const int m = line0 + line, r = tree_row(a, m), h = g * a.group + m - r * a.group;
+  const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + b * a.qs[0] + r * a.qs[1] + h * a.qs[2] + c * 8;
+  if (vec) {
+    w = *reinterpret_cast<const uint4*>(q);
+  } else {
+    auto two = [&](int e) { return (uint32_t)__bfloat16_as_ushort(q[e]) | (uint32_t)__bfloat16_as_ushort(q[e + 1]) << 16; };
+    w = make_uint4(two(0), two(2), two(4), two(6));
   }
+}
+template <int N, bool Q8>
+__device__ __forceinline__ void tree_store_q(int item, const uint4& v, uint8_t* Qs, float* rs) {    // (whole warps)
+  const int line = item >> 4, c = item & 15;
+  if (!Q8) {
+    *reinterpret_cast<uint4*>(Qs + (c >> 3) * (N * 128) + line * 128 + (((c & 7) ^ (line & 7)) << 4)) = v;
+    return;
+  }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t top = 0;     // magnitudes order as their patterns do
+#pragma unroll
+  for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+#pragma unroll
+  for (int s = 8; s >= 1; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+  const int ex = max((int)(top >> 7), 20) - 127;            // of the largest magnitude
+  const float f = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+  if (c == 0) rs[line] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)(127 - 7 + ex) << 23);
+  uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
+    const uint32_t h = tree_e4m3x2(x0, x1);
+    const float2 r = __half22float2(tree_half2(h));
+    hi[e >> 1] |= h << (16 * (e & 1));
+    lo[e >> 1] |= tree_e4m3x2(x0 - r.x, x1 - r.y) << (16 * (e & 1));
+  }
+  uint8_t* at = Qs + line * 128 + (((c >> 1) ^ (line & 7)) << 4) + (c & 1) * 8;
+  *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
+  *reinterpret_cast<uint2*>(at + N * 128) = make_uint2(lo[0], lo[1]);
 }
 
 // Address of the 16-byte piece of row rr of a V^T tile: pieces of 16 (e4m3) or 8 keys
@@ -231,7 +237,7 @@ __device__ __forceinline__ uint4* tree_v_piece(uint8_t* tile, int rr, int piece)
 
 // Values of drafted keys (in the tile: from .. to - 1) that are not finite: cleared, and their keys noted
 template <bool Q8>
-__device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison) {
+__device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison, int* poisoned) {
   constexpr int KPP = Q8 ? 16 : 8, KPW = Q8 ? 4 : 2;     // keys of a piece, of a word
   const int lane = threadIdx.x & 31;
   for (int pc = from / KPP; pc * KPP < to; ++pc)
@@ -252,6 +258,7 @@ __device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, in
               const int j = key - from + first_draft;
               atomicOr(&poison[j >> 5], 1u << (j & 31));
               any = true;
+              *poisoned = 1;
             }
           }
         }
@@ -276,8 +283,9 @@ __global__ void __launch_bounds__(TreeTc<N, Q8>::kThreads, TreeTc<N, Q8>::kResid
 k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a, const int vec_q) {
   using C = TreeTc<N, Q8>;
   extern __shared__ uint8_t smem_tree[];
-  const int b = blockIdx.z, R = a.rows[b], G = a.group, nkv = a.c.n_kv_heads;
-  const int g = blockIdx.y % nkv, line0 = blockIdx.y / nkv * N, n = min(N, R * G - line0);
+  const int g = blockIdx.y, G = a.group, nkv = a.c.n_kv_heads;
+  const int b = a.line_tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / a.line_tiles, line0 = ((int)blockIdx.z - b * a.line_tiles) * N;
+  const int R = a.rows[b], n = min(N, R * G - line0);
   const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
   if (n <= 0 || T <= 0) return;
@@ -290,14 +298,64 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     return;
   }
 
+  // the queries are asked for before the tiles of all CTAs fill the way from memory
+  uint4 q0, q1;
+  tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, threadIdx.x, q0);
+  if (threadIdx.x + C::kThreads < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, threadIdx.x + C::kThreads, q1);
+  // softmax warps: who sees this thread's key, a bit for each of the warp's lines: tiles without drafted keys by the keys' number
+  // alone, the (at most three) others by the mask; and the scales of this thread's key in the tile to come
+  const int draft0 = ctx / kTreeTile;
+  uint32_t seen[3], of_line[3];
+  float ks = 0.f, vs = 1.f;
+  const float* k_scale = nullptr;
+  const float* v_scale = nullptr;
+  if (warp >= 4) {
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * kTreeCols, line = line0 + col0 + (lane & 15);
+    const uint32_t* row = a.mask && line < line0 + n ? a.mask + ((size_t)b * a.max_rows + tree_row(a, line)) * a.words : nullptr;
+    if (Q8) {
+      const size_t at = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + quarter * 32 + lane;
+      k_scale = a.c.k_scale + at; v_scale = a.c.v_scale + at;
+      if (tile0 * kTreeTile + quarter * 32 + lane < keys) { ks = *k_scale; vs = *v_scale; }
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {      // lane = line: the 32 keys of the warp's quarter
+      const int jd = (draft0 + i) * kTreeTile + quarter * 32 - ctx, w = jd >> 5;
+      const bool here = draft0 + i >= tile0 && draft0 + i < tile0 + T;
+      auto word = [&](int x) { return row && here && x >= 0 && x < a.words ? row[x] : 0xffffffffu; };
+      of_line[i] = __funnelshift_r(word(w), word(w + 1), jd & 31);
+      if (R - jd < 32) of_line[i] &= R - jd > 0 ? (1u << (R - jd)) - 1u : 0u;
+    }
+  }
+  // a tile of K or of V^T into its slot (one thread)
+  const int krow = (b * nkv + g) * a.c.max_ctx, vrow = (b * nkv + g) * kHd;
+  auto load_k = [&](int j) {
+    const int s = j % C::kRingK, key = (tile0 + j) * kTreeTile;
+    uint8_t* dst = kring + (size_t)s * C::kSlot;
+    ptx::mbar_expect_tx(&c.k_full[s], C::kSlot);
+    ptx::tma_load_2d(dst, &map_k, &c.k_full[s], 0, krow + key);
+    if (!Q8) ptx::tma_load_2d(dst + kSub, &map_k, &c.k_full[s], 64, krow + key);
+  };
+  auto load_v = [&](int j) {
+    const int s = j % C::kRingV, key = (tile0 + j) * kTreeTile;
+    uint8_t* dst = vring + (size_t)s * C::kSlot;
+    ptx::mbar_expect_tx(&c.v_full[s], C::kSlot);
+    ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
+    if (!Q8) ptx::tma_load_2d(dst + kSub, &map_v, &c.v_full[s], key + 64, vrow);
+  };
   if (threadIdx.x == 0) {
-    c.abort_flag = 0; c.late_flag = 0;
+    c.abort_flag = 0; c.late_flag = 0; c.poisoned = 0;
     for (int i = 0; i < C::kRingK; ++i) { ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1); }
     for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
     ptx::mbar_init(&c.p_full, 4 * C::kGroups);       // the softmax warps
     ptx::mbar_init(&c.p_empty, 1);
     ptx::fence_barrier_init();
+    ptx::fence_proxy_async_smem();
+    // the first tiles are on their way while the CTA sets up (the slots are free)
+    for (int j = 0; j < T && j < max(C::kRingK, C::kRingV); ++j) {
+      if (j < C::kRingK) load_k(j);
+      if (j < C::kRingV) load_v(j);
+    }
   }
   if (threadIdx.x < 8) c.poison[threadIdx.x] = 0u;
   if (threadIdx.x < N) c.nm[0][threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
@@ -305,8 +363,18 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
   }
-  if (vec_q) tree_queries<N, Q8, true>(a, b, g, line0, n, Qs, c.rs);
-  else tree_queries<N, Q8, false>(a, b, g, line0, n, Qs, c.rs);
+  tree_store_q<N, Q8>(threadIdx.x, q0, Qs, c.rs);
+  if (threadIdx.x + C::kThreads < N * 16) tree_store_q<N, Q8>(threadIdx.x + C::kThreads, q1, Qs, c.rs);   // (whole warps)
+  if (warp >= 4) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      seen[i] = 0xffff0000u;
+      if (draft0 + i >= tile0 && draft0 + i < tile0 + T) {
+#pragma unroll
+        for (int e = 0; e < kTreeCols; ++e) seen[i] |= ((__shfl_sync(0xffffffffu, of_line[i], e) >> lane) & 1u) << e;
+      }
+    }
+  }
   ptx::fence_proxy_async_smem();
   ptx::tc_fence_before();
   __syncthreads();
@@ -315,7 +383,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   pdl_trigger();   // (the join; not before the allocation: pdl.cuh)
 
   int* abort_flag = &c.abort_flag;
-  int loads = 0;   // of the producer thread: tiles of K and of V^T, in turn
+  int loads_k = 0, loads_v = 0;   // of the producer thread
   auto valid_keys = [&](int j) { return min(kTreeTile, keys - (tile0 + j) * kTreeTile); };
   // V^T tiles that are put in order before their product: the stretch's last ones
   auto drafted = [&](int j) { return a.mask && (tile0 + j) * kTreeTile + valid_keys(j) > ctx; };
@@ -323,23 +391,16 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer ----------------
-      const int krow = (b * nkv + g) * a.c.max_ctx, vrow = (b * nkv + g) * kHd;
-      for (int j = 0; j < T; ++j) {
-        int s = j % C::kRingK;
-        const int key = (tile0 + j) * kTreeTile;
-        if (!tree_wait(&c.k_empty[s], ((uint32_t)(j / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
-        uint8_t* dst = kring + (size_t)s * C::kSlot;
-        ptx::mbar_expect_tx(&c.k_full[s], C::kSlot);
-        ptx::tma_load_2d(dst, &map_k, &c.k_full[s], 0, krow + key);
-        if (!Q8) ptx::tma_load_2d(dst + kSub, &map_k, &c.k_full[s], 64, krow + key);
-        ++loads;
-        s = j % C::kRingV;
-        if (!tree_wait(&c.v_empty[s], ((uint32_t)(j / C::kRingV) & 1u) ^ 1u, abort_flag)) break;
-        dst = vring + (size_t)s * C::kSlot;
-        ptx::mbar_expect_tx(&c.v_full[s], C::kSlot);
-        ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
-        if (!Q8) ptx::tma_load_2d(dst + kSub, &map_v, &c.v_full[s], key + 64, vrow);
-        ++loads;
+      loads_k = min(T, C::kRingK); loads_v = min(T, C::kRingV);
+      while (loads_k < T || loads_v < T) {
+        if (loads_k < T) {
+          if (!tree_wait(&c.k_empty[loads_k % C::kRingK], ((uint32_t)(loads_k / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
+          load_k(loads_k++);
+        }
+        if (loads_v < T) {
+          if (!tree_wait(&c.v_empty[loads_v % C::kRingV], ((uint32_t)(loads_v / C::kRingV) & 1u) ^ 1u, abort_flag)) break;
+          load_v(loads_v++);
+        }
       }
     }
   } else if (warp == 1 || warp == 2) {
@@ -363,7 +424,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
               if (Q8) tree_clear_v8(tile, rr, valid);
               else attn_clear_v(tile, rr, valid);
             }
-          if (drafted(j)) tree_clean_v<Q8>(tile, max(0, ctx - key0), valid, max(0, key0 - ctx), c.poison);
+          if (drafted(j)) tree_clean_v<Q8>(tile, max(0, ctx - key0), valid, max(0, key0 - ctx), c.poison, &c.poisoned);
           ptx::fence_proxy_async_smem();
           __syncwarp();
         }
@@ -408,34 +469,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     const int ng = min(CW, n - col0);               // lines of this group (0 and less: none)
     const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
     const int bar = 1 + group;                      // named barrier of the group's four warps
-    // who sees this thread's key, a bit for each line: tiles without drafted keys by the keys' number alone, the (at most
-    // three) others by the mask
-    const int draft0 = ctx / kTreeTile;
-    uint32_t seen[3];
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const int tile = draft0 + i, jd = tile * kTreeTile + key - ctx;
-      seen[i] = jd < R ? 0xffffffffu : 0u;
-      if (a.mask && jd >= 0 && jd < R && tile >= tile0 && tile < tile0 + T) {
-        const uint32_t* col = a.mask + (size_t)b * a.max_rows * a.words + (jd >> 5);
-        uint32_t w = 0;
-        int r = (line0 + col0) / G, left = G - (line0 + col0) % G;    // lines left of row r
-#pragma unroll 8
-        for (int e = 0; e < ng; ++e) {
-          w |= ((col[(size_t)r * a.words] >> (jd & 31)) & 1u) << e;
-          if (--left == 0) { ++r; left = G; }
-        }
-        seen[i] = w;
-      }
-    }
-    const float* k_scale = nullptr;
-    const float* v_scale = nullptr;
-    float ks = 0.f, vs = 1.f;      // of this thread's key in the tile to come
-    if (Q8) {
-      const size_t at = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + key;
-      k_scale = a.c.k_scale + at; v_scale = a.c.v_scale + at;
-      if (key < valid_keys(0)) { ks = k_scale[0]; vs = v_scale[0]; }
-    }
     // this key's row of P: 16-byte pieces of 16 (8) lines, exchanged by the swizzle of rows of 32, 64 or 128 bytes
     const uint32_t p_row = ptx::smem_u32(Ps) + (uint32_t)(key * C::kPRow);
     const int p_turn = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
@@ -488,17 +521,21 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       ptx::tc_fence_after();
       const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
       float v[CW];
-      ptx::tmem_ld_32x16(s_col, v);
-      ptx::tmem_ld_wait();
-      exponents(v, c.nm[cur], mul, lv, sees);
-      float most = -INFINITY;
+      bool move = j == 0;      // (there is no maximum yet)
+      if (!move) {
+        ptx::tmem_ld_32x16(s_col, v);
+        ptx::tmem_ld_wait();
+        exponents(v, c.nm[cur], mul, lv, sees);
+        float most = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < CW; i += 8) {
-        if (i >= ng) break;
+        for (int i = 0; i < CW; i += 8) {
+          if (i >= ng) break;
 #pragma unroll
-        for (int e = i; e < i + 8; e += 2) most = ptx::fmax3(most, v[e], v[e + 1]);
+          for (int e = i; e < i + 8; e += 2) most = ptx::fmax3(most, v[e], v[e + 1]);
+        }
+        move = !ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)));
       }
-      if (!ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)))) {
+      if (move) {
         // ---- the maxima move: from the scores themselves, over the group's four warps ----
         ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
@@ -508,12 +545,16 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           v[i] = i < ng && ((sees >> i) & 1u) ? u : -INFINITY;
         }
         const int col = col0 + (lane & 15);
-        const float part = tree_reduce<true>(v, lane);
-        if (lane < 16) c.part[quarter][col] = part;
+#pragma unroll
+        for (int i = 0; i < CW; ++i) {
+          const float top = tree_max(v[i]);
+          if (lane == i) c.part[quarter][col] = top;
+        }
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
         const float old = -c.nm[cur][col];
-        const float now = fmaxf(fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col])), old);
-        const float f = old == -INFINITY ? 0.f : exp2f(old - now);
+        const float top = fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col]));
+        const float now = fmaxf(top + (Q8 ? kAhead : 0.f), old);
+        const float f = old == -INFINITY ? 0.f : attn_ex2(old - now);
         if (quarter == 0 && lane < 16) c.nm[cur ^ 1][col] = -now;
         if (j > 0) {   // O^T: all products so far are in
           ok = ok && __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
@@ -590,7 +631,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     float sum[CW];
 #pragma unroll
     for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
-    const float part = tree_reduce<false>(sum, lane);
+    const float part = tree_sum(sum, lane);
     if (lane < 16) {
       c.part[quarter][col0 + lane] = part;
       if (quarter == 0) c.rs[col0 + lane] = -c.nm[cur][col0 + lane];     // (for the output below)
@@ -620,37 +661,39 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       }
       // lane = line: its sum, whether it sees a key that is not finite, its place
       float l = 0.f;
+      long long at = 0;
       if (lane < ng) {
-        const int col = col0 + lane, m = line0 + col, r = m / G, h = g * G + m % G;
+        const int col = col0 + lane, m = line0 + col, r = tree_row(a, m), h = g * G + m - r * G;
         l = (c.part[0][col] + c.part[1][col]) + (c.part[2][col] + c.part[3][col]);
         bool bad = failed;
-        if (a.mask)
+        if (c.poisoned)
           for (int w = 0; w < a.words; ++w)
             if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
         if (bad) l = __uint_as_float(0x7fffffffu);
-        if (!alone && quarter == 0)
-          a.part_ml[(size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)] = make_float2(c.rs[col], l);
+        const long long line = (long long)blockIdx.x * a.lines + tree_line(a, b, r, h);
+        if (!alone && quarter == 0) a.part_ml[line] = make_float2(c.rs[col], l);
+        at = alone ? b * a.os[0] + r * a.os[1] + h * a.os[2] : line * kHd;
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
-      int r = (line0 + col0) / G, i_in = (line0 + col0) % G;
+      const int dim = quarter * 32 + lane;
 #pragma unroll
       for (int i = 0; i < CW; ++i) {
         if (i >= ng) break;
-        const float w = __shfl_sync(0xffffffffu, inv, i);
-        const int h = g * G + i_in, dim = quarter * 32 + lane;
-        if (alone)
-          static_cast<__nv_bfloat16*>(a.o)[b * a.os[0] + r * a.os[1] + h * a.os[2] + dim] = __float2bfloat16_rn(w == 0.f ? 0.f : o[i] * w);
-        else
-          a.part_o[((size_t)blockIdx.x * a.lines + tree_line(a, b, r, h)) * kHd + dim] = o[i];
-        if (++i_in == G) { i_in = 0; ++r; }
+        const long long to = __shfl_sync(0xffffffffu, at, i) + dim;
+        if (alone) {
+          const float w = __shfl_sync(0xffffffffu, inv, i);
+          static_cast<__nv_bfloat16*>(a.o)[to] = __float2bfloat16_rn(w == 0.f ? 0.f : o[i] * w);
+        } else {
+          a.part_o[to] = o[i];
+        }
       }
     }
   }
-  if (loads > 0 && c.abort_flag != 0) {
+  if (loads_k > 0 && c.abort_flag != 0) {
     // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)
-    for (int j = max(0, (loads + 1) / 2 - C::kRingK); j < (loads + 1) / 2; ++j)
+    for (int j = max(0, loads_k - C::kRingK); j < loads_k; ++j)
       tree_wait(&c.k_full[j % C::kRingK], (uint32_t)(j / C::kRingK) & 1u, &c.late_flag);
-    for (int j = max(0, loads / 2 - C::kRingV); j < loads / 2; ++j)
+    for (int j = max(0, loads_v - C::kRingV); j < loads_v; ++j)
       tree_wait(&c.v_full[j % C::kRingV], (uint32_t)(j / C::kRingV) & 1u, &c.late_flag);
   }
   ptx::tc_fence_before();

@@ -111,7 +111,7 @@ template <typename T, typename H>
 bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
   static std::atomic<unsigned long long> done;
   if (!opt_in(k_tree_simt<T, H>, tree_simt_smem(256), done)) return false;
-  k_tree_simt<T, H><<<dim3(p.joined, p.line_tiles * a.c.n_kv_heads, batch), 128, tree_simt_smem(a.c.head_dim), s>>>(a);
+  k_tree_simt<T, H><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), 128, tree_simt_smem(a.c.head_dim), s>>>(a);
   return true;
 }
 
@@ -123,7 +123,7 @@ bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, cudaS
   CUtensorMap mk, mv;
   const uint64_t heads = (uint64_t)a.c.max_batch * a.c.n_kv_heads;
   if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
-  k_tree_tc<N, Q8><<<dim3(p.joined, p.line_tiles * a.c.n_kv_heads, batch), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q);
+  k_tree_tc<N, Q8><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q);
   return true;
 }
 
@@ -156,7 +156,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   if (p.lines == 0) return DC_OK;
   if (p.bytes && (!in->workspace || !op_aligned(in->workspace) || in->workspace_bytes < p.bytes))
     return op_fail(DC_ERR_INVALID_ARG, "the workspace needs %llu bytes on a 16-byte boundary", (unsigned long long)p.bytes);
-  if ((long long)p.line_tiles * cache->n_kv_heads > 65535) return op_fail(DC_ERR_UNSUPPORTED, "too many kv heads");
+  if (cache->n_kv_heads > 65535 || (long long)p.line_tiles * in->batch > 65535) return op_fail(DC_ERR_UNSUPPORTED, "too many heads");
   TreeArgs a;
   a.c = *cache;
   const size_t layer = (size_t)in->layer * cache->max_batch * cache->n_kv_heads * cache->max_ctx;   // keys
@@ -166,7 +166,8 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.q = in->q; a.o = in->o;
   for (int i = 0; i < 3; ++i) { a.qs[i] = in->q_stride[i]; a.os[i] = in->o_stride[i]; }
   a.mask = in->mask; a.max_rows = in->max_rows; a.words = (in->max_rows + 31) / 32;
-  a.nq = in->n_q_heads; a.group = in->n_q_heads / cache->n_kv_heads;
+  a.nq = in->n_q_heads; a.group = in->n_q_heads / cache->n_kv_heads; a.line_tiles = p.line_tiles;
+  a.group_inv = (uint32_t)((1ull << 32) / a.group + 1);
   a.scale_log2 = (in->scale > 0.f ? in->scale : 1.f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
   a.tiles = p.tiles; a.joined = p.joined; a.lines = p.lines;
   for (int b = 0; b < DC_MAX_BATCH; ++b) {

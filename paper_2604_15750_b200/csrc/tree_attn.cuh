@@ -19,7 +19,8 @@ struct TreeArgs {
   long long qs[3], os[3];        // sequence, row, head
   const uint32_t* mask;
   int words, max_rows;
-  int nq, group;
+  int nq, group, line_tiles;
+  uint32_t group_inv;            // floor(2^32 / group) + 1: quotients of lines by the group without a division (tree_row)
   float scale_log2;              // scale * log2(e)
   int tiles;                     // of a stretch
   int joined;                    // stretches of the longest sequence; 1: none is written down
@@ -35,6 +36,8 @@ __device__ __forceinline__ int tree_stretches(const TreeArgs& a, int b) {
   const int t = (a.ctx[b] + a.rows[b] + kTreeTile - 1) / kTreeTile;
   return (t + a.tiles - 1) / a.tiles;
 }
+// row of line m: m / group, exactly where m * group < 2^32 (a sequence has 2^19 lines at most, a group 2^11)
+__device__ __forceinline__ int tree_row(const TreeArgs& a, int m) { return a.group == 1 ? m : (int)__umulhi((uint32_t)m, a.group_inv); }
 // place of (sequence, row, query head) among the lines
 __device__ __forceinline__ int tree_line(const TreeArgs& a, int b, int r, int h) { return a.base[b] + r * a.nq + h; }
 
@@ -49,6 +52,7 @@ __global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeA
   const int n = tree_stretches(a, b);
   if (n <= 1) return;            // (its unit has written the output)
   const int r = (line - a.base[b]) / a.nq, h = (line - a.base[b]) % a.nq;
+  // lane = stretch (32 at a time); a stretch without a key that the row sees has m = -infinity and sums of 0
   float top = -INFINITY;
   for (int s = lane; s < n; s += 32) top = fmaxf(top, a.part_ml[(size_t)s * a.lines + line].x);
 #pragma unroll
@@ -56,16 +60,25 @@ __global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeA
   float o[8], l = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = 0.f;
-  for (int s = 0; s < n; ++s) {
-    const size_t at = (size_t)s * a.lines + line;
-    const float2 ml = a.part_ml[at];
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;    // no key of this stretch is seen
-    const float w = exp2f(ml.x - top);
-    l = fmaf(w, ml.y, l);
+  for (int s0 = 0; s0 < n; s0 += 32) {
+    float w = 0.f;
+    if (s0 + lane < n) {
+      const float2 ml = a.part_ml[(size_t)(s0 + lane) * a.lines + line];
+      w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+      l = fmaf(w, ml.y, ml.x == -INFINITY ? l + ml.y : l);     // (NaN without a maximum: a NaN score, or a wait that ran out)
+    }
+    const int m = min(32, n - s0);
+#pragma unroll 4
+    for (int s = 0; s < m; ++s) {
+      const float ws = __shfl_sync(0xffffffffu, w, s);
+      const float* from = a.part_o + ((size_t)(s0 + s) * a.lines + line) * hd + lane;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i * 32 + lane < hd) o[i] = fmaf(w, a.part_o[at * hd + i * 32 + lane], o[i]);
+      for (int i = 0; i < 8; ++i)
+        if (i * 32 + lane < hd) o[i] = fmaf(ws, from[i * 32], o[i]);
+    }
   }
+#pragma unroll
+  for (int i = 16; i >= 1; i >>= 1) l += __shfl_xor_sync(0xffffffffu, l, i);
   T* dst = static_cast<T*>(a.o) + b * a.os[0] + r * a.os[1] + h * a.os[2];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -73,7 +86,7 @@ __global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeA
 }
 
 // ---- CUDA cores: any head_dim and alignment, fp32 ----------------------------------------------------------
-// grid (stretch, kv head * line tiles, sequence); 4 warps of 4 lines.  Scores: a lane takes a key; products with V: a lane
+// grid (stretch, kv head, sequence * line tiles); 4 warps of 4 lines.  Scores: a lane takes a key; products with V: a lane
 // takes dims.
 constexpr int kTreeLines = 16, kTreeKeys = 32;
 __host__ __device__ inline int tree_simt_smem(int hd) { return (kTreeLines * hd + kTreeKeys * (hd + 1) + hd * (kTreeKeys + 1)) * 4; }
@@ -81,8 +94,8 @@ __host__ __device__ inline int tree_simt_smem(int hd) { return (kTreeLines * hd 
 template <typename T, typename H>
 __global__ void __launch_bounds__(128) k_tree_simt(const __grid_constant__ TreeArgs a) {
   extern __shared__ float tree_smem[];
-  const int b = blockIdx.z, R = a.rows[b], G = a.group, hd = a.c.head_dim, nkv = a.c.n_kv_heads;
-  const int g = blockIdx.y % nkv, line0 = blockIdx.y / nkv * kTreeLines;
+  const int b = blockIdx.z / a.line_tiles, R = a.rows[b], G = a.group, hd = a.c.head_dim, nkv = a.c.n_kv_heads;
+  const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kTreeLines;
   const int keys = a.ctx[b] + R, k0 = blockIdx.x * a.tiles * kTreeTile, k1 = min(keys, k0 + a.tiles * kTreeTile);
   if (line0 >= R * G || k0 >= keys) return;
   float *qs = tree_smem, *ks = qs + kTreeLines * hd, *vs = ks + kTreeKeys * (hd + 1);
