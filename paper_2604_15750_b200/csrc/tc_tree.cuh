@@ -60,9 +60,10 @@ struct TreeCtl {
   uint32_t tmem_base;
   int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
-  alignas(16) float nm[2][N];            // the lines' maxima, negative (log2 units): the current set and the one before
+  alignas(16) float nm[N];               // the lines' maxima, negative (log2 units)
+  alignas(16) float fac[N];              // what the sums are scaled by when they move
   alignas(16) float rs[N];               // e4m3: 2^e of a line's q
-  float part[4][N];
+  alignas(16) float part[4][N];
 };
 
 // Sum of v[col] over the lanes of a warp, 16 columns at once: lane i returns that of column i % 16.
@@ -79,6 +80,15 @@ __device__ __forceinline__ float tree_sum(float (&v)[16], int lane) {
     }
   }
   return v[0];
+}
+// 32 lanes x 4 consecutive columns of TMEM
+__device__ __forceinline__ void tree_tmem_ld4(uint32_t at, float (&v)[4]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tree_tmem_st4(uint32_t at, float x, float y, float z, float w) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
+               ::"r"(at), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)), "r"(__float_as_uint(z)), "r"(__float_as_uint(w)) : "memory");
 }
 // largest value of a warp, NaN passed over
 __device__ __forceinline__ float tree_max(float x) {
@@ -358,7 +368,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     }
   }
   if (threadIdx.x < 8) c.poison[threadIdx.x] = 0u;
-  if (threadIdx.x < N) c.nm[0][threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
+  if (threadIdx.x < N) c.nm[threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
   if (warp == 1) {
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
@@ -502,7 +512,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         }
       }
     };
-    int cur = 0;
     bool ok = true;
     for (int j = 0; j < T; ++j) {
       const int tile = tile0 + j, d = tile - draft0;
@@ -525,7 +534,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (!move) {
         ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
-        exponents(v, c.nm[cur], mul, lv, sees);
+        exponents(v, c.nm, mul, lv, sees);
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < CW; i += 8) {
@@ -536,53 +545,51 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         move = !ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)));
       }
       if (move) {
-        // ---- the maxima move: from the scores themselves, over the group's four warps ----
-        ptx::tmem_ld_32x16(s_col, v);
-        ptx::tmem_ld_wait();
+        // ---- the maxima move: from the scores themselves, over the group's four warps.  Loops over 4 lines that stay
+        // loops: this code runs once or a few times, and what it costs is its way from memory ----
+#pragma unroll 1
+        for (int i = 0; i < CW; i += 4) {
+          float u[4];
+          tree_tmem_ld4(s_col + i, u);
+          ptx::tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < CW; ++i) {
-          const float u = fmaf(Q8 ? v[i] * c.rs[col0 + i] : v[i], mul, lv);
-          v[i] = i < ng && ((sees >> i) & 1u) ? u : -INFINITY;
+          for (int e = 0; e < 4; ++e) {
+            u[e] = fmaf(Q8 ? u[e] * c.rs[col0 + i + e] : u[e], mul, lv);
+            u[e] = tree_max((sees >> (i + e)) & 1u ? u[e] : -INFINITY);
+          }
+          if (lane == 0) *reinterpret_cast<float4*>(&c.part[quarter][col0 + i]) = make_float4(u[0], u[1], u[2], u[3]);
         }
-        const int col = col0 + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < CW; ++i) {
-          const float top = tree_max(v[i]);
-          if (lane == i) c.part[quarter][col] = top;
+        if (j > 0)   // O^T: all products so far are in
+          ok = ok && __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+        ok = ptx::all_agree(bar, 128, ok);
+        if (!ok) break;
+        if (quarter == 0 && lane < CW) {
+          const int col = col0 + lane;
+          const float top = fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col]));
+          const float old = -c.nm[col], now = fmaxf(top + (Q8 ? kAhead : 0.f), old);
+          c.nm[col] = -now;                            // (of columns without a line it stays infinite)
+          c.fac[col] = old == -INFINITY ? 0.f : attn_ex2(old - now);
         }
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
-        const float old = -c.nm[cur][col];
-        const float top = fmaxf(fmaxf(c.part[0][col], c.part[1][col]), fmaxf(c.part[2][col], c.part[3][col]));
-        const float now = fmaxf(top + (Q8 ? kAhead : 0.f), old);
-        const float f = old == -INFINITY ? 0.f : attn_ex2(old - now);
-        if (quarter == 0 && lane < 16) c.nm[cur ^ 1][col] = -now;
-        if (j > 0) {   // O^T: all products so far are in
-          ok = ok && __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
-        }
-        ok = ptx::all_agree(bar, 128, ok);
-        cur ^= 1;
-        if (!ok) break;
-#pragma unroll
-        for (int i = 0; i < CW / 2; ++i)
-          acc[i] = tree_mul2(acc[i], ptx::f2_pack(__shfl_sync(0xffffffffu, f, 2 * i), __shfl_sync(0xffffffffu, f, 2 * i + 1)));
         if (j > 0) {
+#pragma unroll
+          for (int i = 0; i < CW / 2; ++i) acc[i] = tree_mul2(acc[i], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
           ptx::tc_fence_after();
-#pragma unroll
-          for (int part_o = 0; part_o < (Q8 ? 2 : 1); ++part_o) {
-            const uint32_t at = t_lane + (uint32_t)(C::kColO + part_o * N);
-            ptx::tmem_ld_32x16(at, v);
+#pragma unroll 1
+          for (int i = 0; i < (Q8 ? 2 * CW : CW); i += 4) {
+            const uint32_t at = t_lane + (uint32_t)(C::kColO + (i & ~(CW - 1)) / CW * N + (i & (CW - 1)));
+            const float4 f = *reinterpret_cast<const float4*>(&c.fac[col0 + (i & (CW - 1))]);
+            float o[4];
+            tree_tmem_ld4(at, o);
             ptx::tmem_ld_wait();
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i] * __shfl_sync(0xffffffffu, f, i));
-            attn_tmem_st16(at, w);
+            tree_tmem_st4(at, o[0] * f.x, o[1] * f.y, o[2] * f.z, o[3] * f.w);
           }
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
         ptx::tmem_ld_32x16(s_col, v);
         ptx::tmem_ld_wait();
-        exponents(v, c.nm[cur], mul, lv, sees);
+        exponents(v, c.nm, mul, lv, sees);
       }
       if (!ok) break;
       ptx::tc_fence_before();
@@ -634,7 +641,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     const float part = tree_sum(sum, lane);
     if (lane < 16) {
       c.part[quarter][col0 + lane] = part;
-      if (quarter == 0) c.rs[col0 + lane] = -c.nm[cur][col0 + lane];     // (for the output below)
+      if (quarter == 0) c.rs[col0 + lane] = -c.nm[col0 + lane];     // (for the output below)
     }
   }
   // ---------------- output ----------------
@@ -644,21 +651,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     constexpr int CW = kTreeCols;
     const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * CW, ng = min(CW, n - col0);
     if (ng > 0) {
-      float o[CW];
-      if (!failed) {
-        const uint32_t at = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
-        ptx::tc_fence_after();
-        ptx::tmem_ld_32x16(at, o);
-        if (Q8) {
-          float lo[CW];
-          ptx::tmem_ld_32x16(at + (uint32_t)N, lo);
-          ptx::tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < CW; ++i) o[i] = fmaf(lo[i], 1.f / 16.f, o[i]) * (1.f / 16.f);
-        } else {
-          ptx::tmem_ld_wait();
-        }
-      }
       // lane = line: its sum, whether it sees a key that is not finite, its place
       float l = 0.f;
       long long at = 0;
@@ -676,15 +668,23 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
       const int dim = quarter * 32 + lane;
+      const uint32_t o_col = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
+      ptx::tc_fence_after();
+#pragma unroll 1
+      for (int i = 0; i < ng; i += 4) {
+        float o[4], lo[4];
+        tree_tmem_ld4(o_col + i, o);        // (whatever is there after a wait that ran out: l is NaN)
+        if (Q8) tree_tmem_ld4(o_col + N + i, lo);
+        ptx::tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < CW; ++i) {
-        if (i >= ng) break;
-        const long long to = __shfl_sync(0xffffffffu, at, i) + dim;
-        if (alone) {
-          const float w = __shfl_sync(0xffffffffu, inv, i);
-          static_cast<__nv_bfloat16*>(a.o)[to] = __float2bfloat16_rn(w == 0.f ? 0.f : o[i] * w);
-        } else {
-          a.part_o[to] = o[i];
+        for (int e = 0; e < 4; ++e) {
+          const long long to = __shfl_sync(0xffffffffu, at, i + e) + dim;
+          const float w = __shfl_sync(0xffffffffu, inv, i + e);
+          if (Q8) o[e] = fmaf(lo[e], 1.f / 16.f, o[e]) * (1.f / 16.f);
+          if (i + e < ng) {
+            if (alone) static_cast<__nv_bfloat16*>(a.o)[to] = __float2bfloat16_rn(w == 0.f ? 0.f : o[e] * w);
+            else a.part_o[to] = o[e];
+          }
         }
       }
     }
