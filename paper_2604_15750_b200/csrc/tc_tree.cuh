@@ -61,7 +61,8 @@ struct TreeCtl {
   int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
   alignas(16) float nm[N];               // the lines' maxima, negative (log2 units)
-  alignas(16) float fac[N];              // what the sums are scaled by when they move
+  alignas(16) float fac[N];              // what the sums are scaled by when they move; at the end 1 / l
+  long long at[N];                       // places of the lines in o or part_o
   alignas(16) float rs[N];               // e4m3: 2^e of a line's q
   alignas(16) float part[4][N];
 };
@@ -245,36 +246,52 @@ __device__ __forceinline__ uint4* tree_v_piece(uint8_t* tile, int rr, int piece)
   return reinterpret_cast<uint4*>(tile + (piece >> 3) * kSub + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4));
 }
 
-// Values of drafted keys (in the tile: from .. to - 1) that are not finite: cleared, and their keys noted
+// Values of drafted keys (in the tile: from .. to - 1) that are not finite: cleared, and their keys noted.  Looked for first, four
+// rows a lane at a time, because they are hardly ever there and the last product waits for this.
 template <bool Q8>
-__device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison, int* poisoned) {
+__device__ __forceinline__ uint32_t tree_not_finite(uint32_t w) {    // top bit of each such value
+  return Q8 ? ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+}
+template <bool Q8>
+__device__ __noinline__ void tree_clear_not_finite(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison) {
   constexpr int KPP = Q8 ? 16 : 8, KPW = Q8 ? 4 : 2;     // keys of a piece, of a word
-  const int lane = threadIdx.x & 31;
   for (int pc = from / KPP; pc * KPP < to; ++pc)
-    for (int rr = lane; rr < 128; rr += 32) {
-      uint4* at = tree_v_piece<Q8>(tile, rr, pc);
-      uint4 w4 = *at;
-      uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-      bool any = false;
-#pragma unroll
+    for (int rr = threadIdx.x & 31; rr < 128; rr += 32) {
+      uint32_t* at = reinterpret_cast<uint32_t*>(tree_v_piece<Q8>(tile, rr, pc));
+#pragma unroll 1
       for (int i = 0; i < 4; ++i) {
-        const uint32_t bad = Q8 ? ((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((w[i] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-        if (bad) {
-#pragma unroll
-          for (int e = 0; e < KPW; ++e) {
-            const int key = pc * KPP + i * KPW + e;
-            if (((bad >> (e * (32 / KPW))) & (Q8 ? 0xffu : 0xffffu)) && key >= from && key < to) {
-              w[i] &= ~((Q8 ? 0xffu : 0xffffu) << (e * (32 / KPW)));
-              const int j = key - from + first_draft;
-              atomicOr(&poison[j >> 5], 1u << (j & 31));
-              any = true;
-              *poisoned = 1;
-            }
+        uint32_t w = at[i];
+        const uint32_t bad = tree_not_finite<Q8>(w);
+        for (int e = 0; e < KPW && bad; ++e) {
+          const int key = pc * KPP + i * KPW + e, j = key - from + first_draft;
+          const uint32_t bits = (Q8 ? 0xffu : 0xffffu) << (e * (32 / KPW));
+          if ((bad & bits) && key >= from && key < to) {
+            w &= ~bits;
+            atomicOr(&poison[j >> 5], 1u << (j & 31));
           }
         }
+        at[i] = w;
       }
-      if (any) *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+template <bool Q8>
+__device__ __forceinline__ void tree_clean_v(uint8_t* tile, int from, int to, int first_draft, uint32_t* poison, int* poisoned) {
+  constexpr int KPP = Q8 ? 16 : 8;
+  const int lane = threadIdx.x & 31;
+  uint32_t any = 0;
+#pragma unroll 1
+  for (int pc = from / KPP; pc * KPP < to; ++pc) {
+    uint4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *tree_v_piece<Q8>(tile, lane + 32 * i, pc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      any |= tree_not_finite<Q8>(w[i].x) | tree_not_finite<Q8>(w[i].y) | tree_not_finite<Q8>(w[i].z) | tree_not_finite<Q8>(w[i].w);
+  }
+  if (__any_sync(0xffffffffu, any != 0)) {     // (it may be of a key of the context, seen by all)
+    tree_clear_not_finite<Q8>(tile, from, to, first_draft, poison);
+    if (lane == 0) *poisoned = 1;
+  }
 }
 
 // Clears keys valid .. up to what the product takes (its steps are 32 keys of e4m3) in row rr
@@ -290,7 +307,7 @@ __device__ __forceinline__ void tree_clear_v8(uint8_t* tile, int rr, int valid) 
 
 template <int N, bool Q8>
 __global__ void __launch_bounds__(TreeTc<N, Q8>::kThreads, TreeTc<N, Q8>::kResident)
-k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a, const int vec_q) {
+k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ TreeArgs a, const int vec_q, const int vec_o) {
   using C = TreeTc<N, Q8>;
   extern __shared__ uint8_t smem_tree[];
   const int g = blockIdx.y, G = a.group, nkv = a.c.n_kv_heads;
@@ -303,15 +320,17 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 96) { ptx::prefetch_tmap(&map_k); ptx::prefetch_tmap(&map_v); }
   if ((ptx::smem_u32(smem_tree) & 1023u) != 0) {   // (it is all the shared memory there is and starts on such a boundary)
     if (threadIdx.x == 0 && a.status) atomicExch(a.status, DC_ERR_UNSUPPORTED);
     return;
   }
 
-  // the queries are asked for before the tiles of all CTAs fill the way from memory
+  // the queries are asked for before the tiles of all CTAs fill the way from memory (by warps 1 ..: warp 0 asks for the tiles)
   uint4 q0, q1;
-  tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, threadIdx.x, q0);
-  if (threadIdx.x + C::kThreads < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, threadIdx.x + C::kThreads, q1);
+  const int item0 = (int)threadIdx.x - 32, item1 = item0 + C::kThreads - 32;
+  if (item0 >= 0 && item0 < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item0, q0);
+  if (item0 >= 0 && item1 < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item1, q1);
   // softmax warps: who sees this thread's key, a bit for each of the warp's lines: tiles without drafted keys by the keys' number
   // alone, the (at most three) others by the mask; and the scales of this thread's key in the tile to come
   const int draft0 = ctx / kTreeTile;
@@ -373,8 +392,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
   }
-  tree_store_q<N, Q8>(threadIdx.x, q0, Qs, c.rs);
-  if (threadIdx.x + C::kThreads < N * 16) tree_store_q<N, Q8>(threadIdx.x + C::kThreads, q1, Qs, c.rs);   // (whole warps)
+  static_assert(N * 16 % 32 == 0 && N * 16 <= 2 * (C::kThreads - 32), "two a thread, in whole warps");
+  if (item0 >= 0 && item0 < N * 16) tree_store_q<N, Q8>(item0, q0, Qs, c.rs);
+  if (item0 >= 0 && item1 < N * 16) tree_store_q<N, Q8>(item1, q1, Qs, c.rs);
   if (warp >= 4) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
@@ -639,55 +659,58 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
 #pragma unroll
     for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
     const float part = tree_sum(sum, lane);
-    if (lane < 16) {
-      c.part[quarter][col0 + lane] = part;
-      if (quarter == 0) c.rs[col0 + lane] = -c.nm[col0 + lane];     // (for the output below)
-    }
+    if (lane < 16) c.part[quarter][col0 + lane] = part;
   }
   // ---------------- output ----------------
   __syncthreads();
-  const bool failed = c.abort_flag != 0, alone = tree_stretches(a, b) == 1;
+  const bool failed = c.abort_flag != 0, alone = a.joined == 1 || tree_stretches(a, b) == 1;
+  // a thread a line: its sum, whether it sees a key that is not finite, its place
+  if ((int)threadIdx.x < n) {
+    const int col = threadIdx.x, m = line0 + col, r = tree_row(a, m), h = g * G + m - r * G;
+    float l = (c.part[0][col] + c.part[1][col]) + (c.part[2][col] + c.part[3][col]);
+    bool bad = failed;
+    if (c.poisoned)
+      for (int w = 0; w < a.words; ++w)
+        if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
+    if (bad) l = __uint_as_float(0x7fffffffu);
+    const long long line = (long long)blockIdx.x * a.lines + tree_line(a, b, r, h);
+    if (!alone) a.part_ml[line] = make_float2(-c.nm[col], l);
+    c.fac[col] = !alone ? 1.f : l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
+    c.at[col] = alone ? b * a.os[0] + r * a.os[1] + h * a.os[2] : line * kHd;
+  }
+  __syncthreads();
+  // O [line][dim] where Q and P were: bf16, or fp32 of a stretch
   if (warp >= 4) {
-    constexpr int CW = kTreeCols;
-    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * CW, ng = min(CW, n - col0);
-    if (ng > 0) {
-      // lane = line: its sum, whether it sees a key that is not finite, its place
-      float l = 0.f;
-      long long at = 0;
-      if (lane < ng) {
-        const int col = col0 + lane, m = line0 + col, r = tree_row(a, m), h = g * G + m - r * G;
-        l = (c.part[0][col] + c.part[1][col]) + (c.part[2][col] + c.part[3][col]);
-        bool bad = failed;
-        if (c.poisoned)
-          for (int w = 0; w < a.words; ++w)
-            if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
-        if (bad) l = __uint_as_float(0x7fffffffu);
-        const long long line = (long long)blockIdx.x * a.lines + tree_line(a, b, r, h);
-        if (!alone && quarter == 0) a.part_ml[line] = make_float2(c.rs[col], l);
-        at = alone ? b * a.os[0] + r * a.os[1] + h * a.os[2] : line * kHd;
-      }
-      const float inv = l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
-      const int dim = quarter * 32 + lane;
-      const uint32_t o_col = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
-      ptx::tc_fence_after();
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * kTreeCols, ng = min(kTreeCols, n - col0), dim = quarter * 32 + lane;
+    const uint32_t o_col = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
+    ptx::tc_fence_after();
 #pragma unroll 1
-      for (int i = 0; i < ng; i += 4) {
-        float o[4], lo[4];
-        tree_tmem_ld4(o_col + i, o);        // (whatever is there after a wait that ran out: l is NaN)
-        if (Q8) tree_tmem_ld4(o_col + N + i, lo);
-        ptx::tmem_ld_wait();
+    for (int i = 0; i < ng; i += 4) {
+      float o[4], lo[4];
+      tree_tmem_ld4(o_col + i, o);        // (whatever is there after a wait that ran out: l is NaN)
+      if (Q8) tree_tmem_ld4(o_col + N + i, lo);
+      ptx::tmem_ld_wait();
+      const float4 f = *reinterpret_cast<const float4*>(&c.fac[col0 + i]);
+      const float ff[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const long long to = __shfl_sync(0xffffffffu, at, i + e) + dim;
-          const float w = __shfl_sync(0xffffffffu, inv, i + e);
-          if (Q8) o[e] = fmaf(lo[e], 1.f / 16.f, o[e]) * (1.f / 16.f);
-          if (i + e < ng) {
-            if (alone) static_cast<__nv_bfloat16*>(a.o)[to] = __float2bfloat16_rn(w == 0.f ? 0.f : o[e] * w);
-            else a.part_o[to] = o[e];
-          }
-        }
+      for (int e = 0; e < 4; ++e) {
+        if (Q8) o[e] = fmaf(lo[e], 1.f / 16.f, o[e]) * (1.f / 16.f);
+        o[e] = ff[e] == 0.f ? 0.f : o[e] * ff[e];
+        if (alone) reinterpret_cast<__nv_bfloat16*>(smem_tree)[(col0 + i + e) * kHd + dim] = __float2bfloat16_rn(o[e]);
+        else reinterpret_cast<float*>(smem_tree)[(col0 + i + e) * kHd + dim] = o[e];
       }
     }
+  }
+  __syncthreads();
+  if (alone && vec_o) {
+    for (int i = threadIdx.x; i < n * 16; i += C::kThreads)
+      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + c.at[i >> 4] + (i & 15) * 8) = reinterpret_cast<const uint4*>(smem_tree)[i];
+  } else if (alone) {
+    for (int i = threadIdx.x; i < n * kHd; i += C::kThreads)
+      static_cast<__nv_bfloat16*>(a.o)[c.at[i >> 7] + (i & 127)] = reinterpret_cast<const __nv_bfloat16*>(smem_tree)[i];
+  } else {
+    for (int i = threadIdx.x; i < n * 32; i += C::kThreads)
+      *reinterpret_cast<float4*>(a.part_o + c.at[i >> 5] + (i & 31) * 4) = reinterpret_cast<const float4*>(smem_tree)[i];
   }
   if (loads_k > 0 && c.abort_flag != 0) {
     // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)

@@ -116,14 +116,14 @@ bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s
 }
 
 template <int N, bool Q8>
-bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, cudaStream_t s) {
+bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, int vec_o, cudaStream_t s) {
   using C = TreeTc<N, Q8>;
   static std::atomic<unsigned long long> done;
   if (!opt_in(k_tree_tc<N, Q8>, C::kSmem, done)) return false;
   CUtensorMap mk, mv;
   const uint64_t heads = (uint64_t)a.c.max_batch * a.c.n_kv_heads;
   if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
-  k_tree_tc<N, Q8><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q);
+  k_tree_tc<N, Q8><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q, vec_o);
   return true;
 }
 
@@ -182,10 +182,10 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
   const int n_lines = p.lines_per_unit == kTreeLines ? 0 : p.lines_per_unit;
-  int vec_q = op_aligned(in->q);
-  for (int i = 0; i < 3; ++i) vec_q = vec_q && in->q_stride[i] % 8 == 0;
-  const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, s) : launch_tc<32, false>(a, p, in->batch, vec_q, s))
-                : n_lines == 64 ? (q8 ? launch_tc<64, true>(a, p, in->batch, vec_q, s) : launch_tc<64, false>(a, p, in->batch, vec_q, s))
+  int vec_q = op_aligned(in->q), vec_o = op_aligned(in->o);
+  for (int i = 0; i < 3; ++i) { vec_q = vec_q && in->q_stride[i] % 8 == 0; vec_o = vec_o && in->o_stride[i] % 8 == 0; }
+  const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<32, false>(a, p, in->batch, vec_q, vec_o, s))
+                : n_lines == 64 ? (q8 ? launch_tc<64, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<64, false>(a, p, in->batch, vec_q, vec_o, s))
                 : f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
                       : (q8 ? launch_simt<__nv_bfloat16, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<__nv_bfloat16, __nv_bfloat16>(a, p, in->batch, s));
   if (!ok) return op_fail(DC_ERR_CUDA, "dc_tree_attention: no shared memory or tensor map");
