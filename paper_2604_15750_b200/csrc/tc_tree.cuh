@@ -182,6 +182,11 @@ __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, volati
   const uint32_t at = ptx::smem_u32(bar);
   return tree_try(at, parity) || tree_wait_on(at, parity, abort_flag);
 }
+// The same for a whole warp, whose lanes agree: the vote keeps the branch of the usual case uniform.
+__device__ __forceinline__ bool tree_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  const uint32_t at = ptx::smem_u32(bar);
+  return __all_sync(0xffffffffu, tree_try(at, parity)) || __all_sync(0xffffffffu, tree_wait_on(at, parity, abort_flag));
+}
 __device__ __forceinline__ float tree_rcp(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -444,7 +449,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int j = 0; j < T && ok; ++j) {
       const int s = pv ? j % C::kRingV : j % C::kRingK;
       if (pv) {
-        ok = __all_sync(0xffffffffu, tree_wait(&c.v_full[s], (uint32_t)(j / C::kRingV) & 1u, abort_flag));
+        ok = tree_wait_warp(&c.v_full[s], (uint32_t)(j / C::kRingV) & 1u, abort_flag);
         if (!ok) break;
         if (drafted(j) || ragged(j)) {     // (while the softmax warps make P)
           const int key0 = (tile0 + j) * kTreeTile, valid = valid_keys(j);
@@ -458,12 +463,11 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           ptx::fence_proxy_async_smem();
           __syncwarp();
         }
-        ok = tree_wait(&c.p_full, (uint32_t)j & 1u, abort_flag);
+        ok = tree_wait_warp(&c.p_full, (uint32_t)j & 1u, abort_flag);
       } else {
-        if (j >= 2) ok = tree_wait(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
-        ok = ok && tree_wait(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
+        if (j >= 2) ok = tree_wait_warp(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
+        ok = ok && tree_wait_warp(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
       }
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       ptx::tc_fence_after();
       if (ptx::elect_one()) {
@@ -496,7 +500,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     // ---------------- softmax: one thread per key of the tile, 16 lines ----------------
     constexpr int CW = kTreeCols;
     const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * CW;
-    const int ng = min(CW, n - col0);               // lines of this group (0 and less: none)
     const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
     const int bar = 1 + group;                      // named barrier of the group's four warps
     // this key's row of P: 16-byte pieces of 16 (8) lines, exchanged by the swizzle of rows of 32, 64 or 128 bytes
@@ -511,7 +514,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       const ptx::f32x2 off2 = ptx::f2_pack(lv + 4.f, lv + 4.f), mul2 = ptx::f2_pack(mul, mul);
 #pragma unroll
       for (int e = 0; e < CW; e += 8) {
-        if (e >= ng) break;
 #pragma unroll
         for (int i = e; i < e + 8; i += 4) {
           const ulonglong2 m2 = *reinterpret_cast<const ulonglong2*>(nm + col0 + i);
@@ -544,7 +546,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         k_scale += kTreeTile; v_scale += kTreeTile;
         if (j + 1 < T && key < valid_keys(j + 1)) { ks = *k_scale; vs = *v_scale; }
       }
-      ok = ok && __all_sync(0xffffffffu, tree_wait(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag));
+      ok = ok && tree_wait_warp(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag);
       // (whatever their waits said, the four warps of a group come to its barriers together: a wait that ran out is a no in the
       // vote on the maxima, and the vote behind it ends the loop for all four)
       ptx::tc_fence_after();
@@ -557,11 +559,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         exponents(v, c.nm, mul, lv, sees);
         float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < CW; i += 8) {
-          if (i >= ng) break;
-#pragma unroll
-          for (int e = i; e < i + 8; e += 2) most = ptx::fmax3(most, v[e], v[e + 1]);
-        }
+        for (int i = 0; i < CW; i += 2) most = ptx::fmax3(most, v[i], v[i + 1]);
         move = !ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)));
       }
       if (move) {
@@ -580,7 +578,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           if (lane == 0) *reinterpret_cast<float4*>(&c.part[quarter][col0 + i]) = make_float4(u[0], u[1], u[2], u[3]);
         }
         if (j > 0)   // O^T: all products so far are in
-          ok = ok && __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+          ok = ok && tree_wait_warp(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag);
         ok = ptx::all_agree(bar, 128, ok);
         if (!ok) break;
         if (quarter == 0 && lane < CW) {
@@ -618,30 +616,22 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       uint32_t hi[8], lo[4];     // bf16: 16 lines; e4m3: 16 lines of each part
       const ptx::f32x2 iv2 = ptx::f2_pack(iv, iv);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) hi[i] = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) lo[i] = 0u;
-#pragma unroll
-      for (int e = 0; e < CW; e += 8) {
-        if (e >= ng) break;
-#pragma unroll
-        for (int i = e; i < e + 8; i += 4) {
-          const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]), p2 = attn_ex2(v[i + 2]), p3 = attn_ex2(v[i + 3]);
-          if (!Q8) {
-            acc[i / 2] = ptx::f2_add(acc[i / 2], ptx::f2_pack(p0, p1));
-            acc[i / 2 + 1] = ptx::f2_add(acc[i / 2 + 1], ptx::f2_pack(p2, p3));
-            const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
-            hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
-            hi[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
-          } else {
-            acc[i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[i / 2]);
-            acc[i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[i / 2 + 1]);
-            tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[i / 4], lo[i / 4]);
-          }
+      for (int i = 0; i < CW; i += 4) {
+        const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]), p2 = attn_ex2(v[i + 2]), p3 = attn_ex2(v[i + 3]);
+        if (!Q8) {
+          acc[i / 2] = ptx::f2_add(acc[i / 2], ptx::f2_pack(p0, p1));
+          acc[i / 2 + 1] = ptx::f2_add(acc[i / 2 + 1], ptx::f2_pack(p2, p3));
+          const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
+          hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
+          hi[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
+        } else {
+          acc[i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[i / 2]);
+          acc[i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[i / 2 + 1]);
+          tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[i / 4], lo[i / 4]);
         }
       }
       // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
-      if (j > 0) ok = __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag));
+      if (j > 0) ok = tree_wait_warp(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag);
       if (!ok) continue;
       auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -654,7 +644,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       if (lane == 0) ptx::mbar_arrive(&c.p_full);
     }
     // O^T is complete once the last P has been read
-    if (ok) ok = __all_sync(0xffffffffu, tree_wait(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag));
+    if (ok) ok = tree_wait_warp(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag);
     float sum[CW];
 #pragma unroll
     for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
