@@ -91,6 +91,18 @@ __device__ __forceinline__ void tree_tmem_st4(uint32_t at, float x, float y, flo
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
                ::"r"(at), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)), "r"(__float_as_uint(z)), "r"(__float_as_uint(w)) : "memory");
 }
+// the same place in the shared memory of another CTA of the cluster
+__device__ __forceinline__ float tree_remote(const float* p, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_shared(ptx::smem_u32(p), (uint32_t)rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 tree_remote4(const void* p, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(ptx::mapa_shared(ptx::smem_u32(p), (uint32_t)rank)) : "memory");
+  return v;
+}
 // largest value of a warp, NaN passed over
 __device__ __forceinline__ float tree_max(float x) {
   float r;
@@ -320,7 +332,11 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int R = a.rows[b], n = min(N, R * G - line0);
   const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
-  if (n <= 0 || T <= 0) return;
+  if (n <= 0) return;                         // (no CTA of the cluster has lines)
+  if (T <= 0) {
+    if (a.cluster) { ptx::cluster_sync(); ptx::cluster_sync(); }
+    return;
+  }
   uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRingK * C::kSlot;
   TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
@@ -653,7 +669,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   }
   // ---------------- output ----------------
   __syncthreads();
-  const bool failed = c.abort_flag != 0, alone = a.joined == 1 || tree_stretches(a, b) == 1;
+  const int stretches = a.joined == 1 ? 1 : tree_stretches(a, b);
+  const bool failed = c.abort_flag != 0, alone = stretches == 1, apart = !alone && !a.cluster;   // apart: k_tree_join joins them
   // a thread a line: its sum, whether it sees a key that is not finite, its place
   if ((int)threadIdx.x < n) {
     const int col = threadIdx.x, m = line0 + col, r = tree_row(a, m), h = g * G + m - r * G;
@@ -664,9 +681,10 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         if (c.poison[w]) bad = bad || (a.mask[((size_t)b * a.max_rows + r) * a.words + w] & c.poison[w]) != 0;
     if (bad) l = __uint_as_float(0x7fffffffu);
     const long long line = (long long)blockIdx.x * a.lines + tree_line(a, b, r, h);
-    if (!alone) a.part_ml[line] = make_float2(-c.nm[col], l);
+    if (apart) a.part_ml[line] = make_float2(-c.nm[col], l);
+    c.rs[col] = l;
     c.fac[col] = !alone ? 1.f : l == 0.f ? 0.f : 1.f / l;      // (NaN stays NaN)
-    c.at[col] = alone ? b * a.os[0] + r * a.os[1] + h * a.os[2] : line * kHd;
+    c.at[col] = apart ? line * kHd : b * a.os[0] + r * a.os[1] + h * a.os[2];
   }
   __syncthreads();
   // O [line][dim] where Q and P were: bf16, or fp32 of a stretch
@@ -698,9 +716,42 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   } else if (alone) {
     for (int i = threadIdx.x; i < n * kHd; i += C::kThreads)
       static_cast<__nv_bfloat16*>(a.o)[c.at[i >> 7] + (i & 127)] = reinterpret_cast<const __nv_bfloat16*>(smem_tree)[i];
-  } else {
+  } else if (apart) {
     for (int i = threadIdx.x; i < n * 32; i += C::kThreads)
       *reinterpret_cast<float4*>(a.part_o + c.at[i >> 5] + (i & 31) * 4) = reinterpret_cast<const float4*>(smem_tree)[i];
+  }
+  if (a.cluster) {
+    // the stretches of these lines are the CTAs of the cluster: each joins some of the lines, a warp a line, from the others' shared memory
+    ptx::cluster_sync();
+    if (!alone) {
+      for (int line = (int)blockIdx.x + warp * stretches; line < n; line += C::kThreads / 32 * stretches) {
+        float m = -INFINITY, l = 0.f;          // lane = stretch
+        if (lane < stretches) {
+          m = -tree_remote(&c.nm[line], lane);
+          l = tree_remote(&c.rs[line], lane);
+        }
+        const float top = tree_max(m), w = m == -INFINITY ? 0.f : attn_ex2(m - top);
+        l = m == -INFINITY ? l : w * l;        // (NaN without a maximum: a NaN score, or a wait that ran out)
+#pragma unroll
+        for (int s = 4; s >= 1; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+        l = __shfl_sync(0xffffffffu, l, 0);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < stretches; ++s) {
+          const float f = __shfl_sync(0xffffffffu, w, s) * inv;
+          const float4 p = tree_remote4(smem_tree + line * (kHd * 4) + lane * 16, s);
+          o.x = fmaf(f, p.x, o.x); o.y = fmaf(f, p.y, o.y); o.z = fmaf(f, p.z, o.z); o.w = fmaf(f, p.w, o.w);
+        }
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x, o.y), hi = __floats2bfloat162_rn(o.z, o.w);
+        __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.o) + c.at[line] + lane * 4;
+        if (vec_o) {
+          *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        } else {
+          to[0] = lo.x; to[1] = lo.y; to[2] = hi.x; to[3] = hi.y;
+        }
+      }
+    }
+    ptx::cluster_sync();      // nobody leaves while another reads its shared memory
   }
   if (loads_k > 0 && c.abort_flag != 0) {
     // given up: what is still on its way lands before another CTA gets this shared memory (with a limit of its own)

@@ -10,16 +10,17 @@ namespace {
 // Units of one call: stretches of `tiles` tiles of keys, `line_tiles` stretches of lines a sequence.
 struct TreePlan {
   int lines_per_unit, slots;
-  int tiles, joined, line_tiles;
+  int tiles, joined, line_tiles, cluster;
   int lines, base[DC_MAX_BATCH];
   uint64_t bytes;
 };
 
 // The stretch that ends first when `slots` units run at once: a unit costs its tiles and a start (barriers, queries, the first
-// loads' latency, the output), and joining costs a launch; both in the time of a tile.
-constexpr int kUnitStart = 2, kJoin = 2;
+// loads' latency, the output), joining costs a cluster's barriers or a launch; all in the time of a tile.
+constexpr int kUnitStart = 4, kJoinCluster = 1, kJoinLaunch = 4;
+constexpr int kMaxCluster = 8;
 
-TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, int slots) {
+TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, int slots, int max_cluster) {
   TreePlan p{};
   p.lines_per_unit = lines_per_unit; p.slots = slots;
   const int G = in->n_q_heads / c->n_kv_heads;
@@ -41,11 +42,12 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, 
     before = t;
     long long n = 0;
     for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * ((tiles[b] + t - 1) / t);
-    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (t < longest ? kJoin : 0);
+    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (t == longest ? 0 : (longest + t - 1) / t <= max_cluster ? kJoinCluster : kJoinLaunch);
     if (best < 0 || cost < best) { best = cost; p.tiles = t; }
   }
   p.joined = longest ? (longest + p.tiles - 1) / p.tiles : 0;
-  if (p.joined > 1) {
+  p.cluster = p.joined > 1 && p.joined <= max_cluster;
+  if (p.joined > 1 && !p.cluster) {
     const uint64_t n = (uint64_t)p.joined * p.lines;
     p.bytes = n * 8 + (n & 1) * 8 + n * c->head_dim * 4;
   }
@@ -76,8 +78,8 @@ int tc_lines(const dc_cache* c, const dc_tree_in* in) {
 
 TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
   const int n = tc_lines(c, in);
-  if (n == 0) return make_plan(c, in, kTreeLines, 2 * sm_count());
-  return make_plan(c, in, n, (n == 32 && c->dtype == DC_E4M3 ? 2 : 1) * sm_count());
+  if (n == 0) return make_plan(c, in, kTreeLines, 2 * sm_count(), 0);
+  return make_plan(c, in, n, (n == 32 && c->dtype == DC_E4M3 ? 2 : 1) * sm_count(), kMaxCluster);
 }
 
 int check(const dc_cache* c, const dc_tree_in* in) {
@@ -102,7 +104,7 @@ bool opt_in(K kernel, int bytes, std::atomic<unsigned long long>& done) {
   cudaGetDevice(&dev);
   const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
   if (done.load(std::memory_order_acquire) & bit) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
   done.fetch_or(bit, std::memory_order_release);
   return true;
 }
@@ -123,8 +125,13 @@ bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, int v
   CUtensorMap mk, mv;
   const uint64_t heads = (uint64_t)a.c.max_batch * a.c.n_kv_heads;
   if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
-  k_tree_tc<N, Q8><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), C::kThreads, C::kSmem, s>>>(mk, mv, a, vec_q, vec_o);
-  return true;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles); cfg.blockDim = dim3(C::kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = p.joined; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr; cfg.numAttrs = p.cluster ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k_tree_tc<N, Q8>, mk, mv, a, vec_q, vec_o) == cudaSuccess;
 }
 
 }  // namespace
@@ -169,7 +176,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.nq = in->n_q_heads; a.group = in->n_q_heads / cache->n_kv_heads; a.line_tiles = p.line_tiles;
   a.group_inv = (uint32_t)((1ull << 32) / a.group + 1);
   a.scale_log2 = (in->scale > 0.f ? in->scale : 1.f / sqrtf((float)cache->head_dim)) * 1.4426950408889634f;
-  a.tiles = p.tiles; a.joined = p.joined; a.lines = p.lines;
+  a.tiles = p.tiles; a.joined = p.joined; a.cluster = p.cluster; a.lines = p.lines;
   for (int b = 0; b < DC_MAX_BATCH; ++b) {
     a.base[b] = b < in->batch ? p.base[b] : 0;
     a.ctx[b] = b < in->batch ? in->ctx_len[b] : 0;
@@ -188,8 +195,11 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
                 : n_lines == 64 ? (q8 ? launch_tc<64, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<64, false>(a, p, in->batch, vec_q, vec_o, s))
                 : f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
                       : (q8 ? launch_simt<__nv_bfloat16, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<__nv_bfloat16, __nv_bfloat16>(a, p, in->batch, s));
-  if (!ok) return op_fail(DC_ERR_CUDA, "dc_tree_attention: no shared memory or tensor map");
-  if (p.joined > 1) {
+  if (!ok) {
+    const cudaError_t e = cudaGetLastError();
+    return op_fail(DC_ERR_CUDA, "dc_tree_attention: %s", e == cudaSuccess ? "no tensor map" : cudaGetErrorString(e));
+  }
+  if (p.joined > 1 && !p.cluster) {
     const dim3 grid((p.lines + 7) / 8);
     if (f32) launch_chained(k_tree_join<float>, grid, dim3(256), 0, s, a, in->batch);
     else launch_chained(k_tree_join<__nv_bfloat16>, grid, dim3(256), 0, s, a, in->batch);

@@ -2,7 +2,7 @@
 //
 // The query rows of one kv head are its "lines": line m is row m / G, head m % G of the group of G = n_q_heads /
 // n_kv_heads that reads it.  A unit of work is (sequence, kv head, a stretch of lines, a stretch of keys); stretches of keys are
-// joined by k_tree_join with the running maximum and sum that each of them leaves:
+// joined - by the CTAs of a cluster or, where they are too many for one, by k_tree_join - with the running maximum and sum that each of them leaves:
 //     m = max_s m_s,   o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s
 #pragma once
 #include "ops.h"
@@ -24,6 +24,7 @@ struct TreeArgs {
   float scale_log2;              // scale * log2(e)
   int tiles;                     // of a stretch
   int joined;                    // stretches of the longest sequence; 1: none is written down
+  int cluster;                   // they are the CTAs of a cluster, which joins them
   int base[DC_MAX_BATCH];        // lines (of all heads) before sequence b: where its partial results are
   int lines;                     // of all sequences
   int ctx[DC_MAX_BATCH], rows[DC_MAX_BATCH];
