@@ -76,8 +76,13 @@ int tc_lines(const dc_cache* c, const dc_tree_in* in) {
   return most * (in->n_q_heads / c->n_kv_heads) <= 32 ? 32 : 64;
 }
 
+bool simt_fast(const dc_cache* c, const dc_tree_in* in) {
+  return (c->head_dim == 64 || (c->head_dim == 128 && in->dtype == DC_F32)) && op_aligned(c->k) && op_aligned(c->v);
+}
+
 TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
   const int n = tc_lines(c, in);
+  if (n == 0 && simt_fast(c, in)) return make_plan(c, in, kSimtLines, 2 * sm_count(), 0);
   if (n == 0) return make_plan(c, in, kTreeLines, 2 * sm_count(), 0);
   return make_plan(c, in, n, (n == 32 && c->dtype == DC_E4M3 ? 2 : 1) * sm_count(), kMaxCluster);
 }
@@ -109,8 +114,20 @@ bool opt_in(K kernel, int bytes, std::atomic<unsigned long long>& done) {
   return true;
 }
 
+template <typename T, typename H, int HD>
+bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
+  static std::atomic<unsigned long long> done;
+  if (!opt_in(k_tree_simt_hd<T, H, HD>, tree_simt_smem_hd(HD), done)) return false;
+  k_tree_simt_hd<T, H, HD><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), 256, tree_simt_smem_hd(HD), s>>>(a);
+  return true;
+}
+
 template <typename T, typename H>
 bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
+  if (p.lines_per_unit == kSimtLines) {
+    if (a.c.head_dim == 64) return launch_simt_hd<T, H, 64>(a, p, batch, s);
+    if constexpr (sizeof(T) == 4) return launch_simt_hd<T, H, 128>(a, p, batch, s);    // (bf16 rows have the tensor cores)
+  }
   static std::atomic<unsigned long long> done;
   if (!opt_in(k_tree_simt<T, H>, tree_simt_smem(256), done)) return false;
   k_tree_simt<T, H><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), 128, tree_simt_smem(a.c.head_dim), s>>>(a);
@@ -188,7 +205,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.status = in->status;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
-  const int n_lines = p.lines_per_unit == kTreeLines ? 0 : p.lines_per_unit;
+  const int n_lines = tc_lines(cache, in);
   int vec_q = op_aligned(in->q), vec_o = op_aligned(in->o);
   for (int i = 0; i < 3; ++i) { vec_q = vec_q && in->q_stride[i] % 8 == 0; vec_o = vec_o && in->o_stride[i] % 8 == 0; }
   const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<32, false>(a, p, in->batch, vec_q, vec_o, s))

@@ -86,6 +86,200 @@ __global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeA
     if (i * 32 + lane < hd) dst[i * 32 + lane] = op_to<T>(l == 0.f ? 0.f : o[i] / l);
 }
 
+// ---- CUDA cores, head_dim 64 or 128, cache on 16-byte boundaries ------------------------------------------
+// grid (stretch, kv head, sequence * line tiles); 256 threads, 32 lines, 64 keys at a time.  In both products a thread has 2 lines x 4
+// keys or 2 lines x HD/16 dims in registers and takes 6 to 10 16-byte loads from shared memory for 32 to 64 multiply-adds.  The next
+// keys are on their way while these are worked on.
+constexpr int kSimtLines = 32, kSimtKeys = 64;
+__host__ __device__ constexpr int tree_simt_smem_hd(int hd) {
+  return (kSimtLines * (hd + 4) + kSimtKeys * (hd + 4) + hd * (kSimtKeys + 4) + kSimtLines * (kSimtKeys + 4)) * 4;
+}
+// 16 bytes of a cache as fp32
+template <typename H> __device__ __forceinline__ void tree_wide(const uint4& w, float (&x)[16 / sizeof(H)]);
+template <> __device__ __forceinline__ void tree_wide<float>(const uint4& w, float (&x)[4]) {
+  x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+}
+template <> __device__ __forceinline__ void tree_wide<__nv_bfloat16>(const uint4& w, float (&x)[8]) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+template <> __device__ __forceinline__ void tree_wide<__nv_fp8_e4m3>(const uint4& w, float (&x)[16]) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    x[2 * i] = f.x; x[2 * i + 1] = f.y;
+  }
+}
+
+template <typename T, typename H, int HD>
+__global__ void __launch_bounds__(256, 2) k_tree_simt_hd(const __grid_constant__ TreeArgs a) {
+  constexpr int E = 16 / sizeof(H);                              // values of a load
+  constexpr int NL = kSimtKeys * HD / E / 256;                   // loads a thread has of K, and of V
+  constexpr int DPT = HD / 16, KP = HD + 4, VP = kSimtKeys + 4;  // dims a thread; row pitches in shared memory
+  extern __shared__ float tree_smem[];
+  __shared__ uint32_t poison[8];
+  const int b = blockIdx.z / a.line_tiles, R = a.rows[b], G = a.group, nkv = a.c.n_kv_heads;
+  const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kSimtLines, n = min(kSimtLines, R * G - line0);
+  const int ctx = a.ctx[b], keys = ctx + R, k0 = blockIdx.x * a.tiles * kTreeTile, k1 = min(keys, k0 + a.tiles * kTreeTile);
+  if (n <= 0 || k0 >= keys) return;
+  float *qs = tree_smem, *ks = qs + kSimtLines * KP, *vs = ks + kSimtKeys * KP, *ps = vs + HD * VP;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;     // keys 4 tx .. + 3 (dims tx, tx + 16, ..) of lines 2 ty, 2 ty + 1
+  const size_t slot = (size_t)b * nkv + g;
+  const H* K = static_cast<const H*>(a.c.k) + slot * a.c.max_ctx * HD;
+  const H* V = static_cast<const H*>(a.c.v) + slot * a.c.max_ctx * HD;
+  const float* k_scale = a.c.k_scale + slot * a.c.max_ctx;
+  const float* v_scale = a.c.v_scale + slot * a.c.max_ctx;
+  uint4 kw[NL], vw[NL];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int j = tid + 256 * i, key = j / (HD / E), d = j / (kSimtKeys / E);
+      kw[i] = t + key < k1 ? *reinterpret_cast<const uint4*>(K + (size_t)(t + key) * HD + j % (HD / E) * E) : make_uint4(0, 0, 0, 0);
+      // (whole pieces: the cache goes on to a multiple of 64 keys)
+      vw[i] = *reinterpret_cast<const uint4*>(V + (size_t)d * a.c.max_ctx + t + j % (kSimtKeys / E) * E);
+    }
+  };
+  fetch(k0);
+  if (tid < 8) poison[tid] = 0;
+  for (int i = tid; i < kSimtLines * HD; i += 256) {
+    const int line = i / HD, m = line0 + line, r = tree_row(a, m);
+    qs[line * KP + i % HD] = line < n ? op_f32(static_cast<const T*>(a.q)[b * a.qs[0] + r * a.qs[1] + (g * G + m - r * G) * a.qs[2] + i % HD]) : 0.f;
+  }
+  const uint32_t* mask[2];
+#pragma unroll
+  for (int l = 0; l < 2; ++l) {
+    const int m = line0 + 2 * ty + l;
+    mask[l] = a.mask && 2 * ty + l < n ? a.mask + ((size_t)b * a.max_rows + tree_row(a, m)) * a.words : nullptr;
+  }
+  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][DPT];
+#pragma unroll
+  for (int l = 0; l < 2; ++l)
+#pragma unroll
+    for (int i = 0; i < DPT; ++i) o[l][i] = 0.f;
+  for (int t = k0; t < k1; t += kSimtKeys) {
+    __syncthreads();
+    const bool drafted = a.mask && t + kSimtKeys > ctx;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int j = tid + 256 * i, key = j / (HD / E), d = j / (kSimtKeys / E), first = j % (kSimtKeys / E) * E;
+      float x[E];
+      tree_wide<H>(kw[i], x);
+      const float sc = sizeof(H) == 1 && t + key < k1 ? k_scale[t + key] : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float4 w = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+        if (sizeof(H) == 1) { w.x *= sc; w.y *= sc; w.z *= sc; w.w *= sc; }
+        *reinterpret_cast<float4*>(ks + key * KP + j % (HD / E) * E + e) = w;
+      }
+      tree_wide<H>(vw[i], x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int at = t + first + e;
+        if (at >= k1) x[e] = 0.f;            // whatever the cache holds there
+        else if (sizeof(H) == 1) x[e] *= v_scale[at];
+        // a drafted key's value that is not finite: 0 times it would be NaN for lines that do not see the key
+        if (drafted && at >= ctx && at < k1 && !(fabsf(x[e]) <= 3.402823466e38f)) {
+          x[e] = 0.f;
+          atomicOr(&poison[(at - ctx) >> 5], 1u << ((at - ctx) & 31));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(vs + d * VP + first + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+    }
+    __syncthreads();
+    if (t + kSimtKeys < k1) fetch(t + kSimtKeys);
+    // scores
+    float z[2][4];
+#pragma unroll
+    for (int l = 0; l < 2; ++l)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[l][e] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < HD; d += 4) {
+      float4 q[2], x[4];
+#pragma unroll
+      for (int l = 0; l < 2; ++l) q[l] = *reinterpret_cast<const float4*>(qs + (2 * ty + l) * KP + d);
+      // (keys tx, tx + 16, ..: neighbours in shared memory rows go to different banks)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(ks + (tx + 16 * e) * KP + d);
+#pragma unroll
+      for (int l = 0; l < 2; ++l)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          z[l][e] = fmaf(q[l].x, x[e].x, fmaf(q[l].y, x[e].y, fmaf(q[l].z, x[e].z, fmaf(q[l].w, x[e].w, z[l][e]))));
+    }
+    // probabilities: the 16 threads of a line pair have its keys
+#pragma unroll
+    for (int l = 0; l < 2; ++l) {
+      float now = top[l];
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = t + tx + 16 * e, j = key - ctx;
+        bool sees = key < k1;
+        if (sees && j >= 0 && mask[l]) sees = (mask[l][j >> 5] >> (j & 31)) & 1u;
+        any = any || sees;
+        z[l][e] = sees ? z[l][e] * a.scale_log2 : -INFINITY;
+        now = fmaxf(now, z[l][e]);
+        ps[(2 * ty + l) * VP + tx + 16 * e] = sees ? 1.f : 0.f;
+      }
+#pragma unroll
+      for (int s = 8; s >= 1; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
+      const float f = top[l] == -INFINITY ? 0.f : exp2f(top[l] - now);
+      sum[l] *= f;
+#pragma unroll
+      for (int i = 0; i < DPT; ++i) o[l][i] *= f;
+      top[l] = now;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float& place = ps[(2 * ty + l) * VP + tx + 16 * e];
+        const float p = place != 0.f ? exp2f(z[l][e] - now) : 0.f;    // (a NaN score stays one)
+        sum[l] += p;
+        place = p;
+      }
+    }
+    __syncwarp();    // (a line's probabilities are made and read by the same half warp)
+#pragma unroll 2
+    for (int k = 0; k < kSimtKeys; k += 4) {
+      float4 p[2];
+#pragma unroll
+      for (int l = 0; l < 2; ++l) p[l] = *reinterpret_cast<const float4*>(ps + (2 * ty + l) * VP + k);
+#pragma unroll
+      for (int i = 0; i < DPT; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(vs + (tx + 16 * i) * VP + k);
+#pragma unroll
+        for (int l = 0; l < 2; ++l) o[l][i] = fmaf(p[l].x, x.x, fmaf(p[l].y, x.y, fmaf(p[l].z, x.z, fmaf(p[l].w, x.w, o[l][i]))));
+      }
+    }
+  }
+  __syncthreads();    // (what the last keys noted)
+  const bool alone = tree_stretches(a, b) == 1;
+#pragma unroll
+  for (int l = 0; l < 2; ++l) {
+    float s = sum[l];
+#pragma unroll
+    for (int i = 8; i >= 1; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
+    if (2 * ty + l >= n) continue;
+    if (mask[l])
+      for (int w = 0; w < a.words; ++w)
+        if (mask[l][w] & poison[w]) s = __uint_as_float(0x7fffffffu);
+    const int m = line0 + 2 * ty + l, r = tree_row(a, m), h = g * G + m - r * G;
+    if (alone) {
+      T* dst = static_cast<T*>(a.o) + b * a.os[0] + r * a.os[1] + h * a.os[2];
+#pragma unroll
+      for (int i = 0; i < DPT; ++i) dst[tx + 16 * i] = op_to<T>(s == 0.f ? 0.f : o[l][i] / s);
+    } else {
+      const size_t at = (size_t)blockIdx.x * a.lines + tree_line(a, b, r, h);
+      if (tx == 0) a.part_ml[at] = make_float2(top[l], s);
+#pragma unroll
+      for (int i = 0; i < DPT; ++i) a.part_o[at * HD + tx + 16 * i] = o[l][i];
+    }
+  }
+}
+
 // ---- CUDA cores: any head_dim and alignment, fp32 ----------------------------------------------------------
 // grid (stretch, kv head, sequence * line tiles); 4 warps of 4 lines.  Scores: a lane takes a key; products with V: a lane
 // takes dims.
