@@ -121,6 +121,28 @@ __device__ __forceinline__ float piece_max(const Piece<float>& p) {
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(p.at(i)) & 0x7fffffffu);
   return __uint_as_float(m);
 }
+// largest magnitude of each of 8 keys over some dims, infinities and NaN on top
+template <int D>
+__device__ __forceinline__ void piece_max_keys(const Piece<__nv_bfloat16> (&p)[D], float (&top)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int d = 0; d < D; ++d) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(p[d].word(i) & 0x7fff7fffu));
+    top[2 * i] = __uint_as_float(m << 16);
+    top[2 * i + 1] = __uint_as_float(m & 0xffff0000u);
+  }
+}
+template <int D>
+__device__ __forceinline__ void piece_max_keys(const Piece<float> (&p)[D], float (&top)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int d = 0; d < D; ++d) m = max(m, __float_as_uint(p[d].at(e)) & 0x7fffffffu);
+    top[e] = __uint_as_float(m);
+  }
+}
 template <typename T>
 __device__ __forceinline__ float piece_max_finite(const Piece<T>& p) {
   float m = 0.f;
@@ -165,20 +187,23 @@ __global__ void __launch_bounds__(kTileThreads) k_rows_tile(const __grid_constan
         }
         Piece<H> y[RPT];
         if constexpr (Q) {
+          float top[RPT];
 #pragma unroll
           for (int j = 0; j < RPT; ++j) {
-            float top = piece_max(x[j]);
+            top[j] = piece_max(x[j]);
+            if (not_finite(top[j])) top[j] = piece_max_finite(x[j]);
 #pragma unroll
-            for (int s = LPR / 2; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-            // (fmaxf passes a NaN over: the vote looks at each lane's own pattern)
-            if (__any_sync(0xffffffffu, not_finite(piece_max(x[j])))) {
-              top = piece_max_finite(x[j]);
+            for (int s = LPR / 2; s >= 1; s >>= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], s));
+          }
+          // lane c makes the scale of row c % RPT for the lanes of its rows (two divisions a lane and not two a row)
+          float mine = top[0];
 #pragma unroll
-              for (int s = LPR / 2; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-            }
-            const float sc = op_scale(top), inv = __fdiv_rn(1.f, sc);
-            const int key = t0 + r0 + j;
-            if (c == 0 && key >= lo && key < hi) scales[key] = sc;
+          for (int j = 1; j < RPT; ++j) mine = c % RPT == j ? top[j] : mine;
+          const float sc = op_scale(mine), inv_mine = __fdiv_rn(1.f, sc);
+          if (c < RPT && t0 + r0 + c >= lo && t0 + r0 + c < hi) scales[t0 + r0 + c] = sc;
+#pragma unroll
+          for (int j = 0; j < RPT; ++j) {
+            const float inv = __shfl_sync(0xffffffffu, inv_mine, j, LPR);
             y[j].w.x = quant2(x[j], 0, inv) | quant2(x[j], 1, inv) << 16;
             y[j].w.y = quant2(x[j], 2, inv) | quant2(x[j], 3, inv) << 16;
           }
@@ -336,11 +361,14 @@ __global__ void __launch_bounds__(kTileThreads) k_rows_tile(const __grid_constan
     if constexpr (Q) {
       float* part = reinterpret_cast<float*>(sh);    // [warp][key]
       float top[8];
+      piece_max_keys(x, top);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        top[e] = 0.f;
+        if (not_finite(top[e])) {
+          top[e] = 0.f;
 #pragma unroll
-        for (int i = 0; i < DPT; ++i) top[e] = fmaxf(top[e], op_magnitude(x[i].at(e)));
+          for (int i = 0; i < DPT; ++i) top[e] = fmaxf(top[e], op_magnitude(x[i].at(e)));
+        }
         top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
         top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16));
       }

@@ -81,6 +81,18 @@ __device__ __forceinline__ void qk_load(const __nv_bfloat16* p, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
 }
+template <typename T> __device__ __forceinline__ void qk_wide(const uint4* w, float (&x)[8]);
+template <> __device__ __forceinline__ void qk_wide<float>(const uint4* w, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    x[4 * i] = __uint_as_float(w[i].x); x[4 * i + 1] = __uint_as_float(w[i].y); x[4 * i + 2] = __uint_as_float(w[i].z); x[4 * i + 3] = __uint_as_float(w[i].w);
+  }
+}
+template <> __device__ __forceinline__ void qk_wide<__nv_bfloat16>(const uint4* w, float (&x)[8]) {
+  const uint32_t u[4] = {w->x, w->y, w->z, w->w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
 __device__ __forceinline__ void qk_store(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
@@ -95,28 +107,43 @@ __device__ __forceinline__ void qk_store(__nv_bfloat16* p, const float (&x)[8]) 
   *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// Units of work are a row and as many of its heads as the CTA has places; a CTA takes every gridDim.x-th one.  The loads of the next
+// unit and its cos and sin are under way while one is worked on.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kQkVecThreads) k_qk_vec(const __grid_constant__ QkArgs a) {
-  constexpr int LPH = HD / 16, HALF = HD / 2;
-  __shared__ __align__(16) float cs[HALF], sn[HALF];
-  const int c = threadIdx.x % LPH * 8, slots = blockDim.x / LPH, heads = a.heads[0] + a.heads[1], t = blockIdx.x;
-  float u[8], v[8];
-  auto load = [&](int j) {
+__global__ void __launch_bounds__(kQkVecThreads, 2) k_qk_vec(const __grid_constant__ QkArgs a, const int passes) {
+  constexpr int LPH = HD / 16, HALF = HD / 2, W = sizeof(T) / 2;      // 16-byte pieces of a lane's half
+  __shared__ __align__(16) float cs[2][HALF], sn[2][HALF];
+  const int c = threadIdx.x % LPH * 8, slots = blockDim.x / LPH, heads = a.heads[0] + a.heads[1];
+  const long long units = (long long)a.rows * passes;
+  uint4 next[2 * W];
+  auto load = [&](long long u) {
+    const int t = passes == 1 ? (int)u : (int)(u / passes), j = (int)(u - (long long)t * passes) * slots + threadIdx.x / LPH;
     if (j < heads) {
       const int w = j >= a.heads[0];
-      const T* x = static_cast<const T*>(a.x[w]) + t * a.xs[w][0] + (w ? j - a.heads[0] : j) * a.xs[w][1];
-      qk_load(x + c, u);
-      qk_load(x + HALF + c, v);
+      const T* x = static_cast<const T*>(a.x[w]) + t * a.xs[w][0] + (w ? j - a.heads[0] : j) * a.xs[w][1] + c;
+#pragma unroll
+      for (int i = 0; i < W; ++i) { next[i] = reinterpret_cast<const uint4*>(x)[i]; next[W + i] = reinterpret_cast<const uint4*>(x + HALF)[i]; }
     }
   };
-  int j = blockIdx.y * slots + threadIdx.x / LPH;
-  load(j);
-  const double p = (double)a.pos[t];
-  for (int i = threadIdx.x; i < HALF; i += blockDim.x) qk_angle(p * a.freq[i], cs[i], sn[i]);
-  __syncthreads();
-  // (every lane stays: the lanes of a head may share a warp with those of a head that is not there)
-  for (int base = blockIdx.y * slots; base < heads; base += gridDim.y * slots, j += gridDim.y * slots) {
-    if (base != (int)blockIdx.y * slots) load(j);
+  auto angles = [&](long long u, int k) {
+    const int t = passes == 1 ? (int)u : (int)(u / passes);
+    const double p = (double)a.pos[t];
+    for (int i = threadIdx.x; i < HALF; i += blockDim.x) qk_angle(p * a.freq[i], cs[k][i], sn[k][i]);
+  };
+  load(blockIdx.x);
+  angles(blockIdx.x, 0);
+  int k = 0;
+  for (long long unit = blockIdx.x; unit < units; unit += gridDim.x, k ^= 1) {
+    __syncthreads();         // (the table of this unit is there, that of the one before has been read)
+    float u[8], v[8];
+    qk_wide<T>(next, u);
+    qk_wide<T>(next + W, v);
+    if (unit + gridDim.x < units) {
+      load(unit + gridDim.x);
+      angles(unit + gridDim.x, k ^ 1);
+    }
+    const int t = passes == 1 ? (int)unit : (int)(unit / passes), j = (int)(unit - (long long)t * passes) * slots + threadIdx.x / LPH;
+    // (every lane stays for the sums: the lanes of a head may share a warp with those of a head that is not there)
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
@@ -131,20 +158,18 @@ __global__ void __launch_bounds__(kQkVecThreads) k_qk_vec(const __grid_constant_
       qk_load(gain + c, y0);
       qk_load(gain + HALF + c, y1);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { y0[i] *= u[i] * r; y1[i] *= v[i] * r; }
+      for (int i = 0; i < 8; ++i) { u[i] *= r * y0[i]; v[i] *= r * y1[i]; }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { y0[i] = u[i] * r; y1[i] = v[i] * r; }
+      for (int i = 0; i < 8; ++i) { u[i] *= r; v[i] *= r; }
     }
-    float cc[8], ss8[8];
-    qk_load(cs + c, cc);
-    qk_load(sn + c, ss8);
+    float cc[8];
+    qk_load(cs[k] + c, cc);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float p0 = y0[i], p1 = y1[i];
-      y0[i] = p0 * cc[i] - p1 * ss8[i];
-      y1[i] = p1 * cc[i] + p0 * ss8[i];
-    }
+    for (int i = 0; i < 8; ++i) { y0[i] = u[i] * cc[i]; y1[i] = v[i] * cc[i]; }
+    qk_load(sn[k] + c, cc);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { y0[i] = fmaf(-v[i], cc[i], y0[i]); y1[i] = fmaf(u[i], cc[i], y1[i]); }
     T* y = static_cast<T*>(a.y[w]) + t * a.ys[w][0] + (w ? j - a.heads[0] : j) * a.ys[w][1];
     qk_store(y + c, y0);
     qk_store(y + HALF + c, y1);
@@ -158,8 +183,9 @@ void launch_vec(const QkArgs& a, cudaStream_t s) {
   // Few rows: the heads of a row are spread over CTAs of a warp or more each, as long as there are SMs without work
   const int spread = max(1, 148 / a.rows);
   const int threads = min(kQkVecThreads, ((heads + spread - 1) / spread * LPH + 31) / 32 * 32);
-  const int slots = threads / LPH;
-  k_qk_vec<T, HD><<<dim3(a.rows, min((heads + slots - 1) / slots, max(spread, 1))), threads, 0, s>>>(a);
+  const int passes = (heads * LPH + threads - 1) / threads;
+  const long long units = (long long)a.rows * passes, most = 148ll * min(2048 / threads, 2 * kQkVecThreads / threads);
+  k_qk_vec<T, HD><<<(int)min(units, most), threads, 0, s>>>(a, passes);
 }
 
 template <typename T>

@@ -217,7 +217,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
     return op_fail(DC_ERR_CUDA, "dc_tree_attention: %s", e == cudaSuccess ? "no tensor map" : cudaGetErrorString(e));
   }
   if (p.joined > 1 && !p.cluster) {
-    const dim3 grid((p.lines + 7) / 8);
+    const dim3 grid(p.lines);
     if (f32) launch_chained(k_tree_join<float>, grid, dim3(256), 0, s, a, in->batch);
     else launch_chained(k_tree_join<__nv_bfloat16>, grid, dim3(256), 0, s, a, in->batch);
   }

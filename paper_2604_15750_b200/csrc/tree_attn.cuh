@@ -42,18 +42,18 @@ __device__ __forceinline__ int tree_row(const TreeArgs& a, int m) { return a.gro
 // place of (sequence, row, query head) among the lines
 __device__ __forceinline__ int tree_line(const TreeArgs& a, int b, int r, int h) { return a.base[b] + r * a.nq + h; }
 
-// ---- joins the stretches: a warp takes one (row, head) --------------------------------------------------
+// ---- joins the stretches: a CTA takes one (row, head), its warps some of the stretches each ---------------------------
+constexpr int kJoinWarps = 8;
 template <typename T>
-__global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeArgs a, const int batch) {
-  pdl_wait();
-  const int lane = threadIdx.x & 31, line = blockIdx.x * 8 + (threadIdx.x >> 5), hd = a.c.head_dim;
-  if (line >= a.lines) return;
+__global__ void __launch_bounds__(32 * kJoinWarps) k_tree_join(const __grid_constant__ TreeArgs a, const int batch) {
+  __shared__ float part[kJoinWarps][256], sum[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, line = blockIdx.x, hd = a.c.head_dim;
   int b = 0;
   while (b + 1 < batch && line >= a.base[b + 1]) ++b;
   const int n = tree_stretches(a, b);
+  pdl_wait();
   if (n <= 1) return;            // (its unit has written the output)
-  const int r = (line - a.base[b]) / a.nq, h = (line - a.base[b]) % a.nq;
-  // lane = stretch (32 at a time); a stretch without a key that the row sees has m = -infinity and sums of 0
+  // a stretch without a key that the row sees has m = -infinity and sums of 0
   float top = -INFINITY;
   for (int s = lane; s < n; s += 32) top = fmaxf(top, a.part_ml[(size_t)s * a.lines + line].x);
 #pragma unroll
@@ -61,29 +61,27 @@ __global__ void __launch_bounds__(256) k_tree_join(const __grid_constant__ TreeA
   float o[8], l = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = 0.f;
-  for (int s0 = 0; s0 < n; s0 += 32) {
-    float w = 0.f;
-    if (s0 + lane < n) {
-      const float2 ml = a.part_ml[(size_t)(s0 + lane) * a.lines + line];
-      w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
-      l = fmaf(w, ml.y, ml.x == -INFINITY ? l + ml.y : l);     // (NaN without a maximum: a NaN score, or a wait that ran out)
-    }
-    const int m = min(32, n - s0);
 #pragma unroll 4
-    for (int s = 0; s < m; ++s) {
-      const float ws = __shfl_sync(0xffffffffu, w, s);
-      const float* from = a.part_o + ((size_t)(s0 + s) * a.lines + line) * hd + lane;
+  for (int s = warp; s < n; s += kJoinWarps) {
+    const size_t at = (size_t)s * a.lines + line;
+    const float2 ml = a.part_ml[at];
+    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+    l = ml.x == -INFINITY ? l + ml.y : fmaf(w, ml.y, l);     // (NaN without a maximum: a NaN score, or a wait that ran out)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i * 32 + lane < hd) o[i] = fmaf(ws, from[i * 32], o[i]);
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i * 32 + lane < hd) o[i] = fmaf(w, a.part_o[at * hd + i * 32 + lane], o[i]);
   }
 #pragma unroll
-  for (int i = 16; i >= 1; i >>= 1) l += __shfl_xor_sync(0xffffffffu, l, i);
-  T* dst = static_cast<T*>(a.o) + b * a.os[0] + r * a.os[1] + h * a.os[2];
+  for (int i = 0; i < 8; ++i) part[warp][i * 32 + lane] = o[i];
+  if (lane == 0) sum[warp] = l;
+  __syncthreads();
+  const int d = threadIdx.x, r = (line - a.base[b]) / a.nq, h = (line - a.base[b]) % a.nq;
+  if (d >= hd) return;
+  float x = 0.f;
+  l = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i * 32 + lane < hd) dst[i * 32 + lane] = op_to<T>(l == 0.f ? 0.f : o[i] / l);
+  for (int w = 0; w < kJoinWarps; ++w) { x += part[w][d]; l += sum[w]; }
+  static_cast<T*>(a.o)[b * a.os[0] + r * a.os[1] + h * a.os[2] + d] = op_to<T>(l == 0.f ? 0.f : x / l);
 }
 
 // ---- CUDA cores, head_dim 64 or 128, cache on 16-byte boundaries ------------------------------------------
