@@ -1,7 +1,10 @@
 // dc_qk_norm_rope: norm of each query and key head and its rotation, one pass over the data.
 #include <math.h>
 
+#include <atomic>
+
 #include "ops.h"
+#include "tc_ptx.cuh"
 
 namespace dc {
 namespace {
@@ -17,11 +20,11 @@ struct QkArgs {
   double freq[128];               // rope_theta^(-2i/hd): radians a position
 };
 
-// cos and sin of pos * freq: the product in fp64, brought into one turn there, then fp32
+// cos and sin of a = pos * freq, the product in fp64: there the fraction of a turn is taken (1 / (2 pi) in two parts), the rest is fp32
 __device__ __forceinline__ void qk_angle(double a, float& c, float& s) {
-  const double turns = rint(a * 0.15915494309189535);                            // 1 / (2 pi)
-  const double r = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, a));   // 2 pi in two parts
-  sincosf((float)r, &s, &c);
+  constexpr double inv = 0.15915494309189535, inv_lo = -9.839338337591243e-18;
+  const double turn = fma(a, inv_lo, fma(a, inv, -rint(a * inv)));
+  sincospif((float)(2.0 * turn), &s, &c);
 }
 
 // Any head_dim, strides and alignment: a warp takes one head; a lane the pairs lane, lane + 32, ..
@@ -69,17 +72,17 @@ __global__ void __launch_bounds__(kQkThreads) k_qk_any(const __grid_constant__ Q
 // head_dim 64, 128 or 256 on 16-byte boundaries: LPH = head_dim / 16 lanes take a head, each 8 pairs (8 dims of the first
 // half, 8 of the second), so that the rotation stays in the lane and the sum of squares takes log2(LPH) shuffles.  A CTA takes a row's
 // heads; their loads are under way while its threads make the row's cos and sin.
-constexpr int kQkVecThreads = 512;
+template <typename T> constexpr int kQkVecThreads = sizeof(T) == 4 ? 256 : 512;      // two or three of these CTAs to an SM
+template <typename T> constexpr int kQkVecCtas = sizeof(T) == 4 ? 3 : 2;
 
-__device__ __forceinline__ void qk_load(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+__device__ __forceinline__ ptx::f32x2 qk_mul2(ptx::f32x2 a, ptx::f32x2 b) {
+  ptx::f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ void qk_load(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+constexpr int kQkDepth = 4;
+__device__ __forceinline__ void qk_copy16(uint4* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
 }
 template <typename T> __device__ __forceinline__ void qk_wide(const uint4* w, float (&x)[8]);
 template <> __device__ __forceinline__ void qk_wide<float>(const uint4* w, float (&x)[8]) {
@@ -107,73 +110,127 @@ __device__ __forceinline__ void qk_store(__nv_bfloat16* p, const float (&x)[8]) 
   *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// Units of work are a row and as many of its heads as the CTA has places; a CTA takes every gridDim.x-th one.  The loads of the next
-// unit and its cos and sin are under way while one is worked on.
+// A thread keeps its head (of the CTA's share blockIdx.y) and goes through every gridDim.x-th row.  The loads of the next rows and the
+// cos and sin of the next one are under way while a row is worked on.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kQkVecThreads, 2) k_qk_vec(const __grid_constant__ QkArgs a, const int passes) {
-  constexpr int LPH = HD / 16, HALF = HD / 2, W = sizeof(T) / 2;      // 16-byte pieces of a lane's half
-  __shared__ __align__(16) float cs[2][HALF], sn[2][HALF];
-  const int c = threadIdx.x % LPH * 8, slots = blockDim.x / LPH, heads = a.heads[0] + a.heads[1];
-  const long long units = (long long)a.rows * passes;
-  uint4 next[2 * W];
-  auto load = [&](long long u) {
-    const int t = passes == 1 ? (int)u : (int)(u / passes), j = (int)(u - (long long)t * passes) * slots + threadIdx.x / LPH;
-    if (j < heads) {
-      const int w = j >= a.heads[0];
-      const T* x = static_cast<const T*>(a.x[w]) + t * a.xs[w][0] + (w ? j - a.heads[0] : j) * a.xs[w][1] + c;
+__global__ void __launch_bounds__(kQkVecThreads<T>, kQkVecCtas<T>) k_qk_vec(const __grid_constant__ QkArgs a) {
+  constexpr int LPH = HD / 16, HALF = HD / 2, W = sizeof(T) / 2, E16 = 16 / sizeof(T);      // W: 16-byte pieces of a lane's half
+  // a row's factors, of queries and of keys: gain and turn in one, y0 = r (u A - v B), y1 = r (v C + u D); a lane's 8 dims are two
+  // 16-byte pieces that lie HALF / 8 pieces apart, so that the lanes of a head read neighbouring pieces
+  __shared__ __align__(16) float tab[2][2][4][HALF];
+  auto place = [](int i) { return ((i >> 2 & 1) * (HALF / 8) + (i >> 3)) * 4 + (i & 3); };
+  const int lane = threadIdx.x % LPH, j = blockIdx.y * (blockDim.x / LPH) + threadIdx.x / LPH, w = j >= a.heads[0];
+  const bool there = j < a.heads[0] + a.heads[1];
+  const int h = there ? (w ? j - a.heads[0] : j) : 0, step = gridDim.x, rows = a.rows;
+  const T* x = static_cast<const T*>(a.x[w]) + blockIdx.x * a.xs[w][0] + h * a.xs[w][1] + lane * 8;
+  T* y = static_cast<T*>(a.y[w]) + blockIdx.x * a.ys[w][0] + h * a.ys[w][1] + lane * 8;
+  const long long x_step = step * a.xs[w][0], y_step = step * a.ys[w][0];
+  // this thread's places in a ring of kQkDepth rows: copies that need no registers while they are on their way, and no barrier,
+  // because a thread reads what it asked for
+  extern __shared__ uint4 qk_ring[];
+  uint4* ring = qk_ring + threadIdx.x;
+  int loaded = blockIdx.x;
+  auto load = [&](int slot) {
+    if (there && loaded < rows) {
 #pragma unroll
-      for (int i = 0; i < W; ++i) { next[i] = reinterpret_cast<const uint4*>(x)[i]; next[W + i] = reinterpret_cast<const uint4*>(x + HALF)[i]; }
+      for (int i = 0; i < W; ++i) {
+        qk_copy16(&ring[(slot * 2 * W + i) * blockDim.x], x + i * E16);
+        qk_copy16(&ring[(slot * 2 * W + W + i) * blockDim.x], x + HALF + i * E16);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    x += x_step;
+    loaded = loaded < rows - step ? loaded + step : rows;
+  };
+  // (HALF threads make the factors: their dim's gains and speed stay in registers)
+  float g[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+  const int dim = threadIdx.x;
+  const double speed = dim < HALF ? a.freq[dim] : 0.0;
+  auto gains = [&](int i, float (&to)[2][2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (a.gain[k]) {
+        to[k][0] = op_f32(static_cast<const T*>(a.gain[k])[i]);
+        to[k][1] = op_f32(static_cast<const T*>(a.gain[k])[i + HALF]);
+      }
+  };
+  auto put = [&](int pos, int k, int i, double freq, const float (&gg)[2][2]) {
+    float c, s;
+    qk_angle((double)pos * freq, c, s);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      tab[k][q][0][place(i)] = gg[q][0] * c; tab[k][q][1][place(i)] = -gg[q][1] * s;
+      tab[k][q][2][place(i)] = gg[q][1] * c; tab[k][q][3][place(i)] = gg[q][0] * s;
     }
   };
-  auto angles = [&](long long u, int k) {
-    const int t = passes == 1 ? (int)u : (int)(u / passes);
-    const double p = (double)a.pos[t];
-    for (int i = threadIdx.x; i < HALF; i += blockDim.x) qk_angle(p * a.freq[i], cs[k][i], sn[k][i]);
+  auto factors = [&](int pos, int k) {
+    if (dim < HALF) put(pos, k, dim, speed, g);
+    for (int i = dim + blockDim.x; i < HALF; i += blockDim.x) {    // (a CTA of fewer threads than pairs: few rows)
+      float more[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+      gains(i, more);
+      put(pos, k, i, a.freq[i], more);
+    }
   };
-  load(blockIdx.x);
-  angles(blockIdx.x, 0);
-  int k = 0;
-  for (long long unit = blockIdx.x; unit < units; unit += gridDim.x, k ^= 1) {
-    __syncthreads();         // (the table of this unit is there, that of the one before has been read)
+#pragma unroll
+  for (int i = 0; i < kQkDepth - 1; ++i) load(i);
+  if (dim < HALF) gains(dim, g);
+  int t = blockIdx.x;
+  factors(a.pos[t], 0);
+  int k = 0, slot = 0, pos = t < rows - step ? a.pos[t + step] : 0;
+  while (true) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kQkDepth - 2) : "memory");
+    __syncthreads();         // (the factors of this row are there, those of the one before have been read)
     float u[8], v[8];
-    qk_wide<T>(next, u);
-    qk_wide<T>(next + W, v);
-    if (unit + gridDim.x < units) {
-      load(unit + gridDim.x);
-      angles(unit + gridDim.x, k ^ 1);
-    }
-    const int t = passes == 1 ? (int)unit : (int)(unit / passes), j = (int)(unit - (long long)t * passes) * slots + threadIdx.x / LPH;
-    // (every lane stays for the sums: the lanes of a head may share a warp with those of a head that is not there)
-    float ss = 0.f;
+    uint4 raw[2 * W];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
+    for (int i = 0; i < 2 * W; ++i) raw[i] = ring[(slot * 2 * W + i) * blockDim.x];
+    qk_wide<T>(raw, u);
+    qk_wide<T>(raw + W, v);
+    load(slot == 0 ? kQkDepth - 1 : slot - 1);      // (the slot of the row before)
+    slot = slot == kQkDepth - 1 ? 0 : slot + 1;
+    const bool more = t < rows - step;
+    if (more) {
+      t += step;
+      factors(pos, k ^ 1);
+      if (t < rows - step) pos = a.pos[t + step];
+    }
+    // (every lane stays for the sums: the lanes of a head may share a warp with those of a head that is not there)
+    ptx::f32x2 u2[4], v2[4], ss2 = 0ull;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u2[i] = ptx::f2_pack(u[2 * i], u[2 * i + 1]);
+      v2[i] = ptx::f2_pack(v[2 * i], v[2 * i + 1]);
+      ss2 = ptx::f2_fma(u2[i], u2[i], ptx::f2_fma(v2[i], v2[i], ss2));
+    }
+    float ss, ss_odd;
+    ptx::f2_unpack(ss2, ss, ss_odd);
+    ss += ss_odd;
 #pragma unroll
     for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-    if (j >= heads) continue;
-    const int w = j >= a.heads[0];
-    const float r = rsqrtf(ss * (1.f / HD) + a.eps);
-    float y0[8], y1[8];
-    if (a.gain[w]) {
-      const T* gain = static_cast<const T*>(a.gain[w]);
-      qk_load(gain + c, y0);
-      qk_load(gain + HALF + c, y1);
+    if (there) {
+      const float r = rsqrtf(ss * (1.f / HD) + a.eps);
+      const ptx::f32x2 r2 = ptx::f2_pack(r, r);
+      float y0[8], y1[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { u[i] *= r * y0[i]; v[i] *= r * y1[i]; }
-    } else {
+      for (int i = 0; i < 4; i += 2) {
+        auto two = [&](int of) { return *reinterpret_cast<const ulonglong2*>(&tab[k][w][of][(i / 2 * (HALF / 8) + lane) * 4]); };
+        const ulonglong2 A = two(0), B = two(1), Cc = two(2), D = two(3);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { u[i] *= r; v[i] *= r; }
+        for (int e = 0; e < 2; ++e) {
+          const ptx::f32x2 ur = qk_mul2(u2[i + e], r2), vr = qk_mul2(v2[i + e], r2);
+          const ptx::f32x2 p = ptx::f2_fma(ur, e ? A.y : A.x, qk_mul2(vr, e ? B.y : B.x)), q = ptx::f2_fma(vr, e ? Cc.y : Cc.x, qk_mul2(ur, e ? D.y : D.x));
+          ptx::f2_unpack(p, y0[2 * (i + e)], y0[2 * (i + e) + 1]);
+          ptx::f2_unpack(q, y1[2 * (i + e)], y1[2 * (i + e) + 1]);
+        }
+      }
+      qk_store(y, y0);
+      qk_store(y + HALF, y1);
     }
-    float cc[8];
-    qk_load(cs[k] + c, cc);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { y0[i] = u[i] * cc[i]; y1[i] = v[i] * cc[i]; }
-    qk_load(sn[k] + c, cc);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { y0[i] = fmaf(-v[i], cc[i], y0[i]); y1[i] = fmaf(u[i], cc[i], y1[i]); }
-    T* y = static_cast<T*>(a.y[w]) + t * a.ys[w][0] + (w ? j - a.heads[0] : j) * a.ys[w][1];
-    qk_store(y + c, y0);
-    qk_store(y + HALF + c, y1);
+    y += y_step;
+    if (!more) break;
+    k ^= 1;
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 template <typename T, int HD>
@@ -182,10 +239,17 @@ void launch_vec(const QkArgs& a, cudaStream_t s) {
   const int heads = a.heads[0] + a.heads[1];
   // Few rows: the heads of a row are spread over CTAs of a warp or more each, as long as there are SMs without work
   const int spread = max(1, 148 / a.rows);
-  const int threads = min(kQkVecThreads, ((heads + spread - 1) / spread * LPH + 31) / 32 * 32);
-  const int passes = (heads * LPH + threads - 1) / threads;
-  const long long units = (long long)a.rows * passes, most = 148ll * min(2048 / threads, 2 * kQkVecThreads / threads);
-  k_qk_vec<T, HD><<<(int)min(units, most), threads, 0, s>>>(a, passes);
+  const int threads = min(kQkVecThreads<T>, ((heads + spread - 1) / spread * LPH + 31) / 32 * 32);
+  const int passes = (heads * LPH + threads - 1) / threads, most = 148 * (kQkVecCtas<T> * kQkVecThreads<T> / threads);
+  const int smem = kQkDepth * sizeof(T) * 16 * threads;
+  static std::atomic<unsigned long long> done;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (!(done.load(std::memory_order_acquire) & bit) &&
+      cudaFuncSetAttribute(k_qk_vec<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQkDepth * sizeof(T) * 16 * kQkVecThreads<T>)) == cudaSuccess)
+    done.fetch_or(bit, std::memory_order_release);
+  k_qk_vec<T, HD><<<dim3(min(a.rows, max(1, most / passes)), passes), threads, smem, s>>>(a);
 }
 
 template <typename T>
