@@ -24,7 +24,7 @@
 //
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
-// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every kTreeCols lines (warp 3
+// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every 16 lines, or 32 of 128 (warp 3
 // has nothing to do: a warp reads the quarter of TMEM's lanes that its number says).
 #pragma once
 #include "tc_attn_parts.cuh"
@@ -32,23 +32,22 @@
 
 namespace dc {
 
-constexpr int kTreeCols = 16;    // lines of a softmax warp
-#ifndef RK
-#define RK 2
-#define RV 3
-#endif
-
 template <int N, bool Q8>
 struct TreeTc {
-  static constexpr int kGroups = N / kTreeCols, kThreads = 128 + 128 * kGroups;
+  static constexpr int kLines = N == 128 ? 32 : 16;             // lines of a softmax warp, in chunks of 16
+  static constexpr int kGroups = N / kLines, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
-  static constexpr int kRingK = Q8 ? (N == 32 ? RK : 4) : 3, kRingV = Q8 ? (N == 32 ? RV : 4) : 3;     // slots of the rings
+  // slots of the rings, as shared memory has room
+  static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : (Q8 ? 4 : 2);
+  static constexpr int kRingV = N == 32 ? 3 : kRingK;
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
-  static constexpr int kCtl = 3072;
+  static constexpr int kCtl = N == 128 ? 8192 : 3072;
   static constexpr int kSmem = 2 * kOperand + (kRingK + kRingV) * kSlot + kCtl;
-  static constexpr int kPRow = Q8 ? N : 2 * N;                  // bytes of a key's row of P (of its hi or lo part): 32, 64 or 128
-  static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : 256;   // TMEM: S^T twice, O^T (its two parts)
+  // P: the rows of the keys, of 128 bytes at most; a second half of the lines lies behind (bf16, 128 lines)
+  static constexpr int kPRow = Q8 ? N : N == 128 ? 128 : 2 * N;
+  static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : N == 64 ? 256 : 512;   // TMEM: S^T twice, O^T (its two parts)
+  static_assert(kColO + (Q8 ? 2 : 1) * N <= kCols && kSmem <= 232448, "TMEM, shared memory");
 };
 // P' of e4m3 is 2^8.8 at most (e4m3 ends at 448): m is set 1 above the maximum, which leaves 5.8 for later tiles, and each time that
 // m moves costs about half a tile.
@@ -210,7 +209,7 @@ __device__ __forceinline__ float tree_lg2(float x) {
   return y;
 }
 
-// Queries of a CTA's lines, 8 dims of a line each, up to two a thread: the loads, and what becomes of them in shared memory (rows of
+// Queries of a CTA's lines, items of 8 dims of a line: the loads, and what becomes of them in shared memory (rows of
 // 128 bytes with the 128-byte swizzle; e4m3: hi, then lo).
 template <int N, bool Q8>
 __device__ __forceinline__ void tree_load_q(const TreeArgs& a, int b, int g, int line0, int n, int vec, int item, uint4& w) {
@@ -348,10 +347,13 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   }
 
   // the queries are asked for before the tiles of all CTAs fill the way from memory (by warps 1 ..: warp 0 asks for the tiles)
-  uint4 q0, q1;
-  const int item0 = (int)threadIdx.x - 32, item1 = item0 + C::kThreads - 32;
-  if (item0 >= 0 && item0 < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item0, q0);
-  if (item0 >= 0 && item1 < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item1, q1);
+  constexpr int kAskers = C::kThreads - 32, kItems = (N * 16 + kAskers - 1) / kAskers;
+  uint4 q[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int item = (int)threadIdx.x - 32 + i * kAskers;
+    if (warp > 0 && item < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item, q[i]);
+  }
   // softmax warps: who sees this thread's key, a bit for each of the warp's lines: tiles without drafted keys by the keys' number
   // alone, the (at most three) others by the mask; and the scales of this thread's key in the tile to come
   const int draft0 = ctx / kTreeTile;
@@ -360,7 +362,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const float* k_scale = nullptr;
   const float* v_scale = nullptr;
   if (warp >= 4) {
-    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * kTreeCols, line = line0 + col0 + (lane & 15);
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * C::kLines, line = line0 + col0 + lane % C::kLines;
     const uint32_t* row = a.mask && line < line0 + n ? a.mask + ((size_t)b * a.max_rows + tree_row(a, line)) * a.words : nullptr;
     if (Q8) {
       const size_t at = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + quarter * 32 + lane;
@@ -408,21 +410,24 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     }
   }
   if (threadIdx.x < 8) c.poison[threadIdx.x] = 0u;
+  static_assert(N <= 128, "a thread a line");
   if (threadIdx.x < N) c.nm[threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
   if (warp == 1) {
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
   }
-  static_assert(N * 16 % 32 == 0 && N * 16 <= 2 * (C::kThreads - 32), "two a thread, in whole warps");
-  if (item0 >= 0 && item0 < N * 16) tree_store_q<N, Q8>(item0, q0, Qs, c.rs);
-  if (item0 >= 0 && item1 < N * 16) tree_store_q<N, Q8>(item1, q1, Qs, c.rs);
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {       // (N * 16 is a multiple of 32: whole warps)
+    const int item = (int)threadIdx.x - 32 + i * kAskers;
+    if (warp > 0 && item < N * 16) tree_store_q<N, Q8>(item, q[i], Qs, c.rs);
+  }
   if (warp >= 4) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      seen[i] = 0xffff0000u;
+      seen[i] = C::kLines == 16 ? 0xffff0000u : 0u;
       if (draft0 + i >= tile0 && draft0 + i < tile0 + T) {
 #pragma unroll
-        for (int e = 0; e < kTreeCols; ++e) seen[i] |= ((__shfl_sync(0xffffffffu, of_line[i], e) >> lane) & 1u) << e;
+        for (int e = 0; e < C::kLines; ++e) seen[i] |= ((__shfl_sync(0xffffffffu, of_line[i], e) >> lane) & 1u) << e;
       }
     }
   }
@@ -458,7 +463,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     // ---------------- issuers of S^T = K Q^T (warp 1) and O^T (+)= V^T P^T (warp 2) ----------------
     const bool pv = warp == 2;
     const uint32_t idesc = tree_idesc<Q8>(N, pv), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
-    const uint32_t b_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs)), ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
+    // (two halves of lines lie 128 rows of 128 bytes apart)
+    const uint32_t b_lo = pv && !Q8 && N == 128 ? (1024u << 16) | ((ptx::smem_u32(Ps) >> 4) & 0x3fffu) : ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs));
+    const uint32_t ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
     // from one product to the next: Q goes on in its row, P by the rows of 16 (32) keys; hi and lo lie behind one another
     const uint32_t b_step = pv ? (uint32_t)((Q8 ? 32 : 16) * C::kPRow >> 4) : 2u, b_half = pv ? 4u * b_step : (uint32_t)(N * 128 >> 4);
     bool ok = true;
@@ -514,40 +521,41 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     }
   } else if (warp >= 4) {
     // ---------------- softmax: one thread per key of the tile, 16 lines ----------------
-    constexpr int CW = kTreeCols;
+    constexpr int CW = C::kLines, QN = CW / 16;     // lines, and chunks of 16 of them
     const int quarter = warp & 3, group = (warp - 4) >> 2, key = quarter * 32 + lane, col0 = group * CW;
     const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col0;
     const int bar = 1 + group;                      // named barrier of the group's four warps
     // this key's row of P: 16-byte pieces of 16 (8) lines, exchanged by the swizzle of rows of 32, 64 or 128 bytes
     const uint32_t p_row = ptx::smem_u32(Ps) + (uint32_t)(key * C::kPRow);
     const int p_turn = C::kPRow == 128 ? key & 7 : C::kPRow == 64 ? (key >> 1) & 3 : (key >> 2) & 1;
-    auto p_piece = [&](int i) { return p_row + (uint32_t)(((group * (Q8 ? 1 : 2) + i) ^ p_turn) << 4); };
-    ptx::f32x2 acc[CW / 2];        // the lines' sums over this thread's keys
+    auto p_piece = [&](int q, int i) {              // piece i of chunk q
+      const int block = group * QN + q;
+      if (Q8) return p_row + (uint32_t)((block ^ p_turn) << 4);
+      return p_row + (uint32_t)(N == 128 ? (block >> 2) * 128 * 128 : 0) + (uint32_t)((((N == 128 ? block & 3 : block) * 2 + i) ^ p_turn) << 4);
+    };
+    ptx::f32x2 acc[QN][8];        // the lines' sums over this thread's keys
 #pragma unroll
-    for (int i = 0; i < CW / 2; ++i) acc[i] = 0ull;
-    // the exponents of P from the scores, -infinity where a line does not see the key
-    auto exponents = [&](float (&v)[CW], const float* nm, float mul, float lv, uint32_t sees) {
+    for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = 0ull;
+    // the exponents of P from the scores of 16 lines, -infinity where a line does not see the key
+    auto exponents = [&](float (&v)[16], int col, float mul, float lv, uint32_t sees) {
       const ptx::f32x2 off2 = ptx::f2_pack(lv + 4.f, lv + 4.f), mul2 = ptx::f2_pack(mul, mul);
 #pragma unroll
-      for (int e = 0; e < CW; e += 8) {
-#pragma unroll
-        for (int i = e; i < e + 8; i += 4) {
-          const ulonglong2 m2 = *reinterpret_cast<const ulonglong2*>(nm + col0 + i);
-          ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
-          if (Q8) {
-            const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col0 + i]);
-            s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
-            s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, m2.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, m2.y));
-          } else {
-            s0 = ptx::f2_fma(s0, mul2, m2.x); s1 = ptx::f2_fma(s1, mul2, m2.y);
-          }
-          ptx::f2_unpack(s0, v[i], v[i + 1]);
-          ptx::f2_unpack(s1, v[i + 2], v[i + 3]);
+      for (int i = 0; i < 16; i += 4) {
+        const ulonglong2 m2 = *reinterpret_cast<const ulonglong2*>(&c.nm[col + i]);
+        ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
+        if (Q8) {
+          const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col + i]);
+          s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
+          s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, m2.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, m2.y));
+        } else {
+          s0 = ptx::f2_fma(s0, mul2, m2.x); s1 = ptx::f2_fma(s1, mul2, m2.y);
         }
-        if (sees != 0xffffffffu) {
+        ptx::f2_unpack(s0, v[i], v[i + 1]);
+        ptx::f2_unpack(s1, v[i + 2], v[i + 3]);
+      }
+      if (sees != 0xffffffffu) {
 #pragma unroll
-          for (int i = e; i < e + 8; ++i) v[i] = (sees >> i) & 1u ? v[i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) v[i] = (sees >> i) & 1u ? v[i] : -INFINITY;
       }
     };
     bool ok = true;
@@ -567,15 +575,22 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       // vote on the maxima, and the vote behind it ends the loop for all four)
       ptx::tc_fence_after();
       const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
-      float v[CW];
+      float v[QN][16];
+      auto scores = [&]() {
+#pragma unroll
+        for (int q = 0; q < QN; ++q) ptx::tmem_ld_32x16(s_col + 16 * q, v[q]);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < QN; ++q) exponents(v[q], col0 + 16 * q, mul, lv, QN == 1 || sees == 0xffffffffu ? sees : (sees >> (16 * q)) | 0xffff0000u);
+      };
       bool move = j == 0;      // (there is no maximum yet)
       if (!move) {
-        ptx::tmem_ld_32x16(s_col, v);
-        ptx::tmem_ld_wait();
-        exponents(v, c.nm, mul, lv, sees);
+        scores();
         float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < CW; i += 2) most = ptx::fmax3(most, v[i], v[i + 1]);
+        for (int q = 0; q < QN; ++q)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) most = ptx::fmax3(most, v[q][i], v[q][i + 1]);
         move = !ptx::all_agree(bar, 128, ok && !(most > (Q8 ? kHeadE4m3 : kHeadBf16)));
       }
       if (move) {
@@ -607,7 +622,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
         if (j > 0) {
 #pragma unroll
-          for (int i = 0; i < CW / 2; ++i) acc[i] = tree_mul2(acc[i], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
+          for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = tree_mul2(acc[i / 8][i % 8], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
           ptx::tc_fence_after();
 #pragma unroll 1
           for (int i = 0; i < (Q8 ? 2 * CW : CW); i += 4) {
@@ -621,51 +636,57 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
-        ptx::tmem_ld_32x16(s_col, v);
-        ptx::tmem_ld_wait();
-        exponents(v, c.nm, mul, lv, sees);
+        scores();
       }
       if (!ok) break;
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.s_empty[j & 1]);
-      uint32_t hi[8], lo[4];     // bf16: 16 lines; e4m3: 16 lines of each part
+      uint32_t hi[QN][8], lo[QN][4];     // bf16: 16 lines; e4m3: 16 lines of each part
       const ptx::f32x2 iv2 = ptx::f2_pack(iv, iv);
 #pragma unroll
-      for (int i = 0; i < CW; i += 4) {
-        const float p0 = attn_ex2(v[i]), p1 = attn_ex2(v[i + 1]), p2 = attn_ex2(v[i + 2]), p3 = attn_ex2(v[i + 3]);
-        if (!Q8) {
-          acc[i / 2] = ptx::f2_add(acc[i / 2], ptx::f2_pack(p0, p1));
-          acc[i / 2 + 1] = ptx::f2_add(acc[i / 2 + 1], ptx::f2_pack(p2, p3));
-          const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
-          hi[i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
-          hi[i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
-        } else {
-          acc[i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[i / 2]);
-          acc[i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[i / 2 + 1]);
-          tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[i / 4], lo[i / 4]);
+      for (int q = 0; q < QN; ++q)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float p0 = attn_ex2(v[q][i]), p1 = attn_ex2(v[q][i + 1]), p2 = attn_ex2(v[q][i + 2]), p3 = attn_ex2(v[q][i + 3]);
+          if (!Q8) {
+            acc[q][i / 2] = ptx::f2_add(acc[q][i / 2], ptx::f2_pack(p0, p1));
+            acc[q][i / 2 + 1] = ptx::f2_add(acc[q][i / 2 + 1], ptx::f2_pack(p2, p3));
+            const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
+            hi[q][i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
+            hi[q][i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
+          } else {
+            acc[q][i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[q][i / 2]);
+            acc[q][i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[q][i / 2 + 1]);
+            tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[q][i / 4], lo[q][i / 4]);
+          }
         }
-      }
       // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
       if (j > 0) ok = tree_wait_warp(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag);
       if (!ok) continue;
       auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
       };
-      st16(p_piece(0), hi[0], hi[1], hi[2], hi[3]);
-      if (Q8) st16(p_piece(0) + 128 * C::kPRow, lo[0], lo[1], lo[2], lo[3]);
-      else st16(p_piece(1), hi[4], hi[5], hi[6], hi[7]);
+#pragma unroll
+      for (int q = 0; q < QN; ++q) {
+        st16(p_piece(q, 0), hi[q][0], hi[q][1], hi[q][2], hi[q][3]);
+        if (Q8) st16(p_piece(q, 0) + 128 * C::kPRow, lo[q][0], lo[q][1], lo[q][2], lo[q][3]);
+        else st16(p_piece(q, 1), hi[q][4], hi[q][5], hi[q][6], hi[q][7]);
+      }
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.p_full);
     }
     // O^T is complete once the last P has been read
     if (ok) ok = tree_wait_warp(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag);
-    float sum[CW];
 #pragma unroll
-    for (int i = 0; i < CW / 2; ++i) ptx::f2_unpack(acc[i], sum[2 * i], sum[2 * i + 1]);
-    const float part = tree_sum(sum, lane);
-    if (lane < 16) c.part[quarter][col0 + lane] = part;
+    for (int q = 0; q < QN; ++q) {
+      float sum[16];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ptx::f2_unpack(acc[q][i], sum[2 * i], sum[2 * i + 1]);
+      const float part = tree_sum(sum, lane);
+      if (lane < 16) c.part[quarter][col0 + 16 * q + lane] = part;
+    }
   }
   // ---------------- output ----------------
   __syncthreads();
@@ -689,7 +710,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   __syncthreads();
   // O [line][dim] where Q and P were: bf16, or fp32 of a stretch
   if (warp >= 4) {
-    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * kTreeCols, ng = min(kTreeCols, n - col0), dim = quarter * 32 + lane;
+    const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * C::kLines, ng = min(C::kLines, n - col0), dim = quarter * 32 + lane;
     const uint32_t o_col = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::kColO + col0);
     ptx::tc_fence_after();
 #pragma unroll 1

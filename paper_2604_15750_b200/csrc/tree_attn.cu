@@ -7,6 +7,19 @@
 namespace dc {
 namespace {
 
+int sm_count() {
+  // (a property of the device; 148 on a B200)
+  static std::atomic<int> n[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 148; }
+  int v = dev < 64 ? n[dev].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); v = 148; }
+    if (dev < 64) n[dev].store(v, std::memory_order_relaxed);
+  }
+  return v;
+}
+
 // Units of one call: stretches of `tiles` tiles of keys, `line_tiles` stretches of lines a sequence.
 struct TreePlan {
   int lines_per_unit, slots;
@@ -54,26 +67,19 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, 
   return p;
 }
 
-int sm_count() {
-  // (a property of the device; 148 on a B200)
-  static std::atomic<int> n[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 148; }
-  int v = dev < 64 ? n[dev].load(std::memory_order_relaxed) : 0;
-  if (v == 0) {
-    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); v = 148; }
-    if (dev < 64) n[dev].store(v, std::memory_order_relaxed);
-  }
-  return v;
-}
-
 // The tensor-core kernel's shapes: N lines of a unit, 0 for the CUDA-core kernel
 int tc_lines(const dc_cache* c, const dc_tree_in* in) {
   const uint64_t keys = (uint64_t)c->max_batch * c->n_kv_heads * c->max_ctx, dims = (uint64_t)c->max_batch * c->n_kv_heads * kHd;
   if (in->dtype != DC_BF16 || c->head_dim != kHd || !op_aligned(c->k) || !op_aligned(c->v) || keys >> 31 || dims >> 31) return 0;
   int most = 0;
   for (int b = 0; b < in->batch; ++b) most = most > in->n_rows[b] ? most : in->n_rows[b];
-  return most * (in->n_q_heads / c->n_kv_heads) <= 32 ? 32 : 64;
+  const int lines = most * (in->n_q_heads / c->n_kv_heads);
+  if (lines <= 64) return lines <= 32 ? 32 : 64;
+  // 128 lines take K and V in half as often and cost less than twice as much, as long as there is work for every SM
+  long long units = 0;
+  for (int b = 0; b < in->batch; ++b)
+    units += (long long)((in->n_rows[b] * (in->n_q_heads / c->n_kv_heads) + 127) / 128) * c->n_kv_heads * ((in->ctx_len[b] + in->n_rows[b] + 8 * kTreeTile - 1) / (8 * kTreeTile));
+  return units >= sm_count() ? 128 : 64;
 }
 
 bool simt_fast(const dc_cache* c, const dc_tree_in* in) {
@@ -209,6 +215,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   int vec_q = op_aligned(in->q), vec_o = op_aligned(in->o);
   for (int i = 0; i < 3; ++i) { vec_q = vec_q && in->q_stride[i] % 8 == 0; vec_o = vec_o && in->o_stride[i] % 8 == 0; }
   const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<32, false>(a, p, in->batch, vec_q, vec_o, s))
+                : n_lines == 128 ? (q8 ? launch_tc<128, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<128, false>(a, p, in->batch, vec_q, vec_o, s))
                 : n_lines == 64 ? (q8 ? launch_tc<64, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<64, false>(a, p, in->batch, vec_q, vec_o, s))
                 : f32 ? (q8 ? launch_simt<float, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<float, float>(a, p, in->batch, s))
                       : (q8 ? launch_simt<__nv_bfloat16, __nv_fp8_e4m3>(a, p, in->batch, s) : launch_simt<__nv_bfloat16, __nv_bfloat16>(a, p, in->batch, s));
