@@ -331,11 +331,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int R = a.rows[b], n = min(N, R * G - line0);
   const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
-  if (n <= 0) return;                         // (no CTA of the cluster has lines)
-  if (T <= 0) {
-    if (a.cluster) { ptx::cluster_sync(); ptx::cluster_sync(); }
-    return;
-  }
+  // (a cluster's barriers wait for the CTAs that are still there, and nobody reads the shared memory of one without keys)
+  if (n <= 0 || T <= 0) return;
   uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRingK * C::kSlot;
   TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");

@@ -53,9 +53,11 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, 
     const int t = (longest + s - 1) / s;
     if (t == before) continue;
     before = t;
+    const int stretches = (longest + t - 1) / t;
+    const bool cluster = stretches > 1 && stretches <= max_cluster;     // (whose places are taken by its CTAs without keys too)
     long long n = 0;
-    for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * ((tiles[b] + t - 1) / t);
-    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (t == longest ? 0 : (longest + t - 1) / t <= max_cluster ? kJoinCluster : kJoinLaunch);
+    for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * (cluster ? stretches : (tiles[b] + t - 1) / t);
+    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (stretches == 1 ? 0 : cluster ? kJoinCluster : kJoinLaunch);
     if (best < 0 || cost < best) { best = cost; p.tiles = t; }
   }
   p.joined = longest ? (longest + p.tiles - 1) / p.tiles : 0;
