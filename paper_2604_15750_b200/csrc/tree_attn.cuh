@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(256, 2) k_tree_simt_hd(const __grid_constant__
     }
     __syncthreads();
     if (t + kSimtKeys < k1) fetch(t + kSimtKeys);
+    if (tid / 32 * 4 >= n) continue;      // (a warp without lines: the others have the pipes for themselves)
     // scores
     float z[2][4];
 #pragma unroll
