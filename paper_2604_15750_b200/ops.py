@@ -61,16 +61,18 @@ def _elsewhere(device, *tensors):
             raise ValueError(f"a tensor is on {t.device}, another on {device}")
 
 
-def _call(f, device, stream, *args):
-    """f(*args, stream) with the tensors' device current."""
-    if device.type != "cuda":
+_current, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _call(f, index, stream, *args):
+    """f(*args, stream) with device `index` current (-1: not a CUDA device)"""
+    if index < 0:
         raise RuntimeError("the operators need tensors on a CUDA device; there is no CPU path")
-    index = device.index
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if index == torch._C._cuda_getDevice():
+    raw = _stream_of(index) if stream is None else stream.cuda_stream
+    if index == _current():
         rc = f(*args, raw)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             rc = f(*args, raw)
     if rc != _b.DC_OK:
         raise _b.DepCapError(rc, _b.lib().dc_last_error(None).decode())
@@ -94,7 +96,7 @@ class KvCache:
         _elsewhere(k.device, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_layers, self.max_batch, self.n_kv_heads, self.max_ctx, self.head_dim = k.shape
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
         self._c = _CACHE.pack(_type(k, "a cache"), *k.shape, k.data_ptr(), v.data_ptr(),
                               0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr())
 
@@ -123,14 +125,14 @@ def _move(f, cache, k, v, pos, n, layer, stream):
     layers, batch, most, heads, hd = k.shape
     if heads != cache.n_kv_heads or hd != cache.head_dim:
         raise ValueError(f"rows of {heads} x {hd} with a cache of {cache.n_kv_heads} x {cache.head_dim}")
-    device = cache.device
-    if k.device != device or v.device != device:
-        _elsewhere(device, k, v)
+    index = cache._index
+    if k.get_device() != index or v.get_device() != index:
+        _elsewhere(cache.device, k, v)
     at, keep = _lengths(pos, batch, "pos")
     n_at, n_keep = _lengths([most] * batch if n is None else n, batch, "n")
-    if max(n_keep.tolist(), default=0) > most:
+    if n is not None and max(n_keep.tolist(), default=0) > most:
         raise ValueError(f"n asks for more than the {most} rows given")
-    _call(f, device, stream, cache._c, _ROWS.pack(batch, layer, layers, _type(k, "rows"), k.data_ptr(), v.data_ptr(), *k.stride(),
+    _call(f, index, stream, cache._c, _ROWS.pack(batch, layer, layers, _type(k, "rows"), k.data_ptr(), v.data_ptr(), *k.stride(),
                                                   *v.stride(), at, n_at))
 
 
@@ -153,14 +155,14 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
     """dc_qk_norm_rope: q [rows, q heads, head_dim], k [rows, kv heads, head_dim] (contiguous dims, else any strides), pos
     int32 [rows] on the device, gains [head_dim] of q's type (None: 1).  Returns q_out, k_out (new ones where None; they may
     be q and k themselves)."""
-    dtype, device, shape, kshape = q.dtype, q.device, q.shape, k.shape
+    dtype, index, shape, kshape = q.dtype, q.get_device(), q.shape, k.shape
     if len(shape) != 3 or len(kshape) != 3 or shape[0] != kshape[0] or shape[2] != kshape[2] or k.dtype != dtype:
         raise ValueError(f"q {tuple(shape)} {dtype}, k {tuple(kshape)} {k.dtype}: [rows, heads, head_dim] of one type")
     rows, hq, hd = shape
     if q_out is None:
-        q_out = torch.empty(shape, dtype=dtype, device=device)
+        q_out = torch.empty(shape, dtype=dtype, device=q.device)
     if k_out is None:
-        k_out = torch.empty(kshape, dtype=dtype, device=device)
+        k_out = torch.empty(kshape, dtype=dtype, device=q.device)
     if q_out.shape != shape or k_out.shape != kshape or q_out.dtype != dtype or k_out.dtype != dtype:
         raise ValueError("an output has another shape or type than its input")
     if pos.dtype != torch.int32 or pos.dim() != 1 or pos.numel() != rows or not pos.is_contiguous():
@@ -170,11 +172,11 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
         if g is None:
             gains.append(0)
             continue
-        if g.dtype != dtype or g.dim() != 1 or g.numel() != hd or not g.is_contiguous() or g.device != device:
-            raise ValueError(f"a gain is a contiguous tensor of {hd} values of {dtype} on {device}")
+        if g.dtype != dtype or g.dim() != 1 or g.numel() != hd or not g.is_contiguous() or g.get_device() != index:
+            raise ValueError(f"a gain is a contiguous tensor of {hd} values of {dtype} on {q.device}")
         gains.append(g.data_ptr())
-    if k.device != device or pos.device != device or q_out.device != device or k_out.device != device:
-        _elsewhere(device, k, pos, q_out, k_out)
+    if not k.get_device() == pos.get_device() == q_out.get_device() == k_out.get_device() == index:
+        _elsewhere(q.device, k, pos, q_out, k_out)
     a, b, d = q.stride()
     e, f, h = k.stride()
     qo, ko = q_out.stride(), k_out.stride()
@@ -185,7 +187,7 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
     x, y, u, w = q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()
     if (x == u and x and qo != (a, b, d)) or (y == w and y and ko != (e, f, h)):
         raise ValueError("an output in the place of its input has the same strides")
-    _call(_b.lib().dc_qk_norm_rope, device, stream,
+    _call(_b.lib().dc_qk_norm_rope, index, stream,
           _QK.pack(_type(q, "q"), rows, hq, kshape[1], hd, eps, rope_theta, x, y, a, b, e, f, *gains, pos.data_ptr(), u, w, qo[0], qo[1],
                    ko[0], ko[1]))
     return q_out, k_out
@@ -196,7 +198,7 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
     n_rows[b] drafted ones behind them.  mask int32 [sequences, rows, (rows + 31) // 32] on the device (`tree_mask`); None: all
     rows of a sequence see one another.  Returns out, like q; its rows >= n_rows[b] are left as they were (zeros in a new one).
     workspace: a uint8 tensor on the device for callers that keep one (`tree_attention_workspace` bytes)."""
-    shape, dtype, device = q.shape, q.dtype, cache.device
+    shape, dtype, index = q.shape, q.dtype, cache._index
     if len(shape) != 4 or shape[3] != cache.head_dim:
         raise ValueError(f"q {tuple(shape)}: sequences, rows, heads, head_dim={cache.head_dim}")
     batch, rows, heads, hd = shape
@@ -220,28 +222,33 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         scale = 0.0
     elif not scale > 0:
         raise ValueError("scale must be positive")
-    if q.device != device or out.device != device or mask is not None or workspace is not None or status is not None:
-        _elsewhere(device, q, out, mask, workspace, status)
+    if q.get_device() != index or out.get_device() != index or workspace is not None or status is not None or \
+            (mask is not None and mask.get_device() != index):
+        _elsewhere(cache.device, q, out, mask, workspace, status)
     ctx, keep = _lengths(ctx_len, batch, "ctx_len")
     n, n_keep = _lengths(n_rows, batch, "n_rows")
     args = (batch, layer, _type(q, "q"), heads, rows, scale, q.data_ptr(), out.data_ptr(), a, b, h, os_[0], os_[1], os_[2], ctx, n, mask_at)
     st = 0 if status is None else status.data_ptr()
-    size = 0
+    call = _b.lib().dc_tree_attention
     if workspace is None:
-        size = _need(cache, _TREE.pack(*args, 0, 0, st))
-        if size:
-            # (of the stream that the work goes to, so that the allocator hands it out again in that order)
-            with nullcontext() if stream is None else torch.cuda.stream(stream):
-                workspace = torch.empty(size, dtype=torch.uint8, device=device)
-    else:
-        size = workspace.numel() * workspace.element_size()
-    _call(_b.lib().dc_tree_attention, device, stream, cache._c, _TREE.pack(*args, workspace.data_ptr() if size else 0, size, st))
+        # most calls want none: whether this one does is asked only after a refusal, which launches nothing
+        try:
+            _call(call, index, stream, cache._c, _TREE.pack(*args, 0, 0, st))
+            return out
+        except _b.DepCapError:
+            size = _need(cache, _TREE.pack(*args, 0, 0, st))
+            if not size:
+                raise
+        # (of the stream that the work goes to, so that the allocator hands it out again in that order)
+        with nullcontext() if stream is None else torch.cuda.stream(stream):
+            workspace = torch.empty(size, dtype=torch.uint8, device=cache.device)
+    _call(call, index, stream, cache._c, _TREE.pack(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
     return out
 
 
 def _need(cache, packed):
     need = C.c_uint64()
-    _call(lambda c, a, stream: _b.lib().dc_tree_attention_workspace(c, a, C.addressof(need)), cache.device, None, cache._c, packed)
+    _call(lambda c, a, stream: _b.lib().dc_tree_attention_workspace(c, a, C.addressof(need)), cache._index, None, cache._c, packed)
     return need.value
 
 
