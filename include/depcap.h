@@ -460,7 +460,8 @@ DC_API int dc_signals_static(const dc_signals_in* in, const dc_signals_out* out,
  * head) is e4m3 values and a scale for all of them:
  *     s = max(a / 448, 2^-80),   a = the largest finite magnitude of the row
  *     held = e4m3(x * (1 / s)) to nearest even, infinities as +-448, NaN as NaN;   it stands for held * s
- * (fp32, each operation rounded).  K and V of a 128-dim row take 264 bytes instead of 512. */
+ * (fp32, each operation rounded).  K and V of a 128-dim row take 264 bytes instead of 512.  Scales that the caller
+ * makes himself are not negative. */
 enum { DC_E4M3 = 2 };    /* dc_cache.dtype, beside DC_F32 and DC_BF16 */
 
 typedef struct dc_cache {
@@ -473,7 +474,7 @@ typedef struct dc_cache {
   float *k_scale, *v_scale; /* device [n_layers][max_batch][n_kv_heads][max_ctx]; DC_E4M3 only, else null */
 } dc_cache;
 
-/* Rows of K and V outside a cache: row r of sequence b (cache slot b) is key pos[b] + r. */
+/* Rows of K and V outside a cache (their memory does not overlap its arrays): row r of sequence b (cache slot b) is key pos[b] + r. */
 typedef struct dc_cache_rows {
   int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
   int32_t layer, n_layers; /* layers layer .. layer + n_layers - 1 of the cache             */
@@ -518,8 +519,8 @@ DC_API int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream);
  * sees all ctx_len[b] keys before them, and drafted key j if bit j of its mask is set (its own key too only by its bit):
  *     o = softmax(scale * q K^T) V    over the keys that it sees; without any, o = 0
  * Query head h uses kv head h / (n_q_heads / n_kv_heads).  What the cache holds at other keys does not matter, NaN included;
- * a row that sees a drafted key whose V has a value that is not finite becomes NaN in every dim, one that does not see it
- * is not touched by it.  Sums and softmax in fp32.  On the tensor cores (bf16 rows, head_dim 128, cache of bf16 or e4m3, arrays
+ * a row that sees a drafted key whose V has a value that is not finite becomes NaN in that dim at least, one that does not
+ * see it is not touched by it.  Sums and softmax in fp32.  On the tensor cores (bf16 rows, head_dim 128, cache of bf16 or e4m3, arrays
  * on 16-byte boundaries) probabilities are rounded to 8 significant bits, as bf16 has. */
 typedef struct dc_tree_in {
   int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
@@ -527,7 +528,7 @@ typedef struct dc_tree_in {
   int32_t dtype;          /* of q and o, DC_F32 | DC_BF16; a cache that is not DC_E4M3 has the same */
   int32_t n_q_heads;      /* a multiple of the cache's n_kv_heads                           */
   int32_t max_rows;       /* 1 .. DC_MAX_WINDOW: row pitch of the mask                      */
-  float scale;            /* 0: 1 / sqrt(head_dim)                                          */
+  float scale;            /* 0: 1 / sqrt(head_dim); at most 1e30                            */
   const void* q;          /* device; the dims of a head are contiguous                      */
   void* o;                /* device; rows >= n_rows[b] are left as they were                */
   int64_t q_stride[3], o_stride[3]; /* sequence, row, head                                  */

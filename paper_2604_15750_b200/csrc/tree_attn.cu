@@ -104,7 +104,7 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   if (in->n_q_heads < 1 || in->n_q_heads % c->n_kv_heads)
     return op_fail(DC_ERR_INVALID_ARG, "%d query heads over %d kv heads", in->n_q_heads, c->n_kv_heads);
   if (in->max_rows < 1 || in->max_rows > DC_MAX_WINDOW) return op_fail(DC_ERR_SHAPE, "max_rows=%d outside [1, %d]", in->max_rows, (int)DC_MAX_WINDOW);
-  if (!(in->scale >= 0.f) || in->scale > 3e38f) return op_fail(DC_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  if (!(in->scale >= 0.f) || in->scale > 1e30f) return op_fail(DC_ERR_INVALID_ARG, "scale outside [0, 1e30]");
   if ((rc = op_check_keys(c, in->batch, in->ctx_len, in->n_rows, in->max_rows, ", max_rows bounds the rows")) != DC_OK) return rc;
   if ((long long)in->max_rows * in->n_q_heads > 524288) return op_fail(DC_ERR_UNSUPPORTED, "more than 524288 rows x query heads");
   return DC_OK;

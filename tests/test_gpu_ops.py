@@ -487,3 +487,98 @@ def test_a_workspace_of_the_callers_own():
     _check_tree(c, 1, q, ctx, rows, bools, out)
     with pytest.raises(dc.DepCapError):
         dc.tree_attention(q.to(DEV), c, ctx, rows, mask.to(DEV), layer=1, workspace=ws[:need - 16])
+
+
+@pytest.mark.parametrize("held", [E4M3, BF16])
+@pytest.mark.parametrize("ctx,rows,hq,hkv", [([5000, 2900], [200, 256], 8, 4), ([4100], [3], 64, 1), ([700, 699], [2, 1], 66, 2)])
+def test_tree_attention_many_lines_of_a_kv_head(held, ctx, rows, hq, hkv):
+    """Over 64 rows x heads of a kv head with work for every SM (128 a CTA), a large group, a group of odd size."""
+    most = max(rows)
+    c, q, mask, bools = _tree_case(BF16, held, ctx, rows, most, hq, hkv, 128, True)
+    out = dc.tree_attention(q.to(DEV), c, ctx, rows, mask.to(DEV), layer=1)
+    _check_tree(c, 1, q, ctx, rows, bools, out)
+
+
+@pytest.mark.parametrize("held,hd", [(E4M3, 128), (BF16, 128), (E4M3, 64)])
+@pytest.mark.parametrize("ctx", [1000, 40000])
+def test_values_that_are_not_finite_in_a_context_cut_into_stretches(held, hd, ctx):
+    """As above, where a cluster (1000 keys) or a second launch (40000) joins the stretches; and K of the same key."""
+    rows = [40]
+    c, q, mask, bools = _tree_case(BF16, held, [ctx], rows, 40, 2, 1, hd, True)
+    ref_out = dc.tree_attention(q.to(DEV), c, [ctx], rows, mask.to(DEV), layer=1)
+    _check_tree(c, 1, q, [ctx], rows, bools, ref_out)
+    for bad_k in (False, True):
+        j = 5
+        x = torch.randn((2, 1, 1, 1, hd), generator=gen(1)).to(BF16)
+        x[0 if bad_k else 1, ..., 3] = math.inf if held == BF16 and not bad_k else math.nan
+        dc.cache_write(c, x[0].to(DEV), x[1].to(DEV), [ctx + j], layer=1)
+        out = dc.tree_attention(q.to(DEV), c, [ctx], rows, mask.to(DEV), layer=1).cpu()
+        for r in range(40):
+            if bools[0, r, j]:
+                assert not torch.isfinite(out[0, r, :, 3]).any()
+            else:
+                assert torch.equal(out[0, r], ref_out[0, r].cpu())
+
+
+def test_keys_with_a_scale_of_zero_count():
+    """A row of zeros that came with a scale of 0 is a key like any other: its probability is in the sum."""
+    ctx, rows = [200], [8]
+    c, q, mask, bools = _tree_case(BF16, E4M3, ctx, rows, 8, 4, 2, 128, True)
+    for t in (c.k, c.k_scale, c.v_scale):
+        raw(t)[1, 0, :, 50:90] = 0
+    raw(c.v)[1, 0, :, :, 50:90] = 0
+    out = dc.tree_attention(q.to(DEV), c, ctx, rows, mask.to(DEV), layer=1)
+    _check_tree(c, 1, q, ctx, rows, bools, out)
+
+
+def test_two_writes_at_once_side_by_side():
+    """Neighbouring keys of one slot written on two streams: no write touches a byte of the other's."""
+    n, cut = 150, 77
+    c = _cache(2, 1, 4, 192, 128, E4M3)
+    x = torch.randn((2, 1, n, 4, 128), generator=gen(1)).to(BF16).to(DEV)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        dc.cache_write(c, x[:, :, :cut], x[:, :, :cut], [3], stream=s1)
+        dc.cache_write(c, x[:, :, cut:], x[:, :, cut:], [3 + cut], stream=s2)
+    torch.cuda.synchronize()
+    held, s = ref.quantised(x[:, 0].transpose(1, 2).cpu())
+    assert torch.equal(raw(c.k[:, 0, :, 3:3 + n]).cpu(), raw(held))
+    assert torch.equal(raw(c.v[:, 0, :, :, 3:3 + n]).cpu(), raw(held).transpose(2, 3))
+    assert torch.equal(c.v_scale[:, 0, :, 3:3 + n].cpu(), s)
+
+
+def test_a_prefilled_context_goes_through_8_bits_into_a_step():
+    """prefill -> 8-bit cache -> the arrays of a step -> step: as with the context rounded on the host."""
+    from paper_2604_15750_b200 import inputs
+    wl = inputs.Workload("ops_bf16", 2, 256, 2, 2, 128, 512, 2048, "bf16", 2, 64, 128, 16, 32, 64, 4243)
+    eng = dc.DepCap.from_workload(wl, inputs.make_weights(wl, DEV), max_last=128)
+    tok = inputs.make_tokens(wl)
+    kv = dc.KvCache.empty(2, 2, 2, 128, 128, BF16, DEV)
+    ids = torch.zeros((2, 128), dtype=torch.int32, device=DEV)
+    ids[:, :120] = tok["prompt"][:, :120].to(DEV)
+    lens = [120, 77]
+    assert not eng.prefill(kv.k, kv.v, ids, lens).any()
+    c = dc.KvCache.empty(2, 2, 2, 192, 128, E4M3, DEV)
+    dc.cache_write(c, *kv.rows(), [0, 0], lens)
+    want_k, want_v = kv.k.clone().cpu(), kv.v.clone().cpu()
+    back = dc.KvCache(kv.k.clone(), kv.v.clone())
+    dc.cache_read(c, *back.rows(), [0, 0], lens)
+    for b, n in enumerate(lens):
+        h, s = ref.quantised(want_k[:, b, :, :n])
+        want_k[:, b, :, :n] = (h.float() * s[..., None]).to(BF16)
+        h, s = ref.quantised(want_v[:, b, :, :, :n].transpose(2, 3))
+        want_v[:, b, :, :, :n] = (h.float() * s[..., None]).to(BF16).transpose(2, 3)
+    assert torch.equal(back.k.cpu(), want_k) and torch.equal(back.v.cpu(), want_v)
+    last = torch.zeros((2, 128), dtype=torch.int32, device=DEV)
+    last[:, :16] = tok["last_ids"].to(DEV)
+    win = tok["win_ids"].to(DEV)
+    res = []
+    for k, v in ((back.k, back.v), (want_k.to(DEV), want_v.to(DEV))):
+        out = eng.step(k, v, lens, last, [16, 16], win, [32, 32], [64, 64])
+        eng.synchronize()
+        res.append({n: out[n].clone() for n in ("pred_id", "conf", "entropy", "influence", "block_len", "status")})
+    assert not res[0]["status"].any()
+    for n in res[0]:
+        assert torch.equal(res[0][n], res[1][n]), n
+    eng.close()

@@ -97,7 +97,7 @@ def test_null_arguments_and_nothing_to_do():
 @pytest.mark.parametrize("bad,code", [
     (dict(dtype=b.DC_E4M3), INVALID), (dict(batch=0), SHAPE), (dict(batch=5), SHAPE), (dict(layer=2), SHAPE), (dict(layer=-1), SHAPE),
     (dict(n_q_heads=3), INVALID), (dict(n_q_heads=0), INVALID), (dict(max_rows=0), SHAPE), (dict(max_rows=257), SHAPE),
-    (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(ctx_len=None), INVALID),
+    (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=1e31), INVALID), (dict(ctx_len=None), INVALID),
     (dict(n_rows=None), INVALID), (dict(ctx_len=ints(-1, 0)), SHAPE), (dict(n_rows=ints(0, 17)), SHAPE), (dict(n_rows=ints(-1, 1)), SHAPE),
     (dict(ctx_len=ints(120, 0), n_rows=ints(9, 0)), SHAPE), (dict(ctx_len=ints(2 ** 31 - 1, 0), n_rows=ints(16, 0)), SHAPE),
     (dict(q=None), INVALID), (dict(o=None), INVALID),
