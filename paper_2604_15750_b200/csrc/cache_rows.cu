@@ -1,5 +1,6 @@
 // dc_cache_write / dc_cache_read: rows of K and V into a cache and back, in 8 bits or as they are.
 #include "ops.h"
+#include "pdl.cuh"
 
 namespace dc {
 namespace {
@@ -17,6 +18,8 @@ constexpr int kAnyWarps = 8;
 
 template <typename T, typename H, bool WRITE>
 __global__ void __launch_bounds__(kAnyWarps * 32) k_rows_any(const RowsArgs a) {
+  pdl_trigger();
+  pdl_wait();
   const int lane = threadIdx.x & 31, nkv = a.c.n_kv_heads, hd = a.c.head_dim;
   const int b = blockIdx.y / nkv, g = blockIdx.y % nkv, side = blockIdx.z & 1, l = blockIdx.z >> 1;
   const long long* st = side ? a.vs : a.ks;
@@ -165,6 +168,8 @@ __global__ void __launch_bounds__(kTileThreads) k_rows_tile(const __grid_constan
   constexpr int RPT = kTk * LPR / kTileThreads;   // rows a thread: 4 (128), 2 (64)
   const int nkv = a.c.n_kv_heads, b = blockIdx.y / nkv, g = blockIdx.y % nkv, side = blockIdx.z & 1, l = blockIdx.z >> 1;
   const int pos = a.pos[b], end = pos + a.n[b], t0 = (pos / kTk + blockIdx.x) * kTk;
+  pdl_trigger();
+  pdl_wait();
   if (t0 >= end) return;
   const int lo = max(pos, t0), hi = min(end, t0 + kTk), tid = threadIdx.x;
   const long long* st = side ? a.vs : a.ks;
@@ -435,17 +440,17 @@ void launch(const RowsArgs& a, int batch, int n_layers, int most, cudaStream_t s
   if (k_ok && (v_rows || v_across)) {
     const dim3 grid(tiles, batch * a.c.n_kv_heads, 2 * n_layers);
     if (v_rows) {
-      if (hd == 128) k_rows_tile<T, H, 128, WRITE, false><<<grid, kTileThreads, 0, s>>>(a);
-      else k_rows_tile<T, H, 64, WRITE, false><<<grid, kTileThreads, 0, s>>>(a);
+      if (hd == 128) launch_chained(k_rows_tile<T, H, 128, WRITE, false>, grid, dim3(kTileThreads), 0, s, a);
+      else launch_chained(k_rows_tile<T, H, 64, WRITE, false>, grid, dim3(kTileThreads), 0, s, a);
     } else {
-      if (hd == 128) k_rows_tile<T, H, 128, WRITE, true><<<grid, kTileThreads, 0, s>>>(a);
-      else k_rows_tile<T, H, 64, WRITE, true><<<grid, kTileThreads, 0, s>>>(a);
+      if (hd == 128) launch_chained(k_rows_tile<T, H, 128, WRITE, true>, grid, dim3(kTileThreads), 0, s, a);
+      else launch_chained(k_rows_tile<T, H, 64, WRITE, true>, grid, dim3(kTileThreads), 0, s, a);
     }
     return;
   }
   // (rows beyond the grid are taken in further turns)
   const dim3 grid(min((most + kAnyWarps - 1) / kAnyWarps, 4096), batch * a.c.n_kv_heads, 2 * n_layers);
-  k_rows_any<T, H, WRITE><<<grid, kAnyWarps * 32, 0, s>>>(a);
+  launch_chained(k_rows_any<T, H, WRITE>, grid, dim3(kAnyWarps * 32), 0, s, a);
 }
 
 template <bool WRITE>

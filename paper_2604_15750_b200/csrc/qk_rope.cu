@@ -4,6 +4,7 @@
 #include <atomic>
 
 #include "ops.h"
+#include "pdl.cuh"
 #include "tc_ptx.cuh"
 
 namespace dc {
@@ -33,6 +34,8 @@ constexpr int kQkThreads = 256;
 template <typename T>
 __global__ void __launch_bounds__(kQkThreads) k_qk_any(const __grid_constant__ QkArgs a) {
   __shared__ float2 turn[128];
+  pdl_trigger();
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = a.hd / 2, heads = a.heads[0] + a.heads[1];
   for (int t = blockIdx.x; t < a.rows; t += gridDim.x) {
     __syncthreads();
@@ -171,6 +174,8 @@ __global__ void __launch_bounds__(kQkVecThreads<T>, kQkVecCtas<T>) k_qk_vec(cons
       put(pos, k, i, a.freq[i], more);
     }
   };
+  pdl_trigger();
+  pdl_wait();
 #pragma unroll
   for (int i = 0; i < kQkDepth - 1; ++i) load(i);
   if (dim < HALF) gains(dim, g);
@@ -249,7 +254,7 @@ void launch_vec(const QkArgs& a, cudaStream_t s) {
   if (!(done.load(std::memory_order_acquire) & bit) &&
       cudaFuncSetAttribute(k_qk_vec<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kQkDepth * sizeof(T) * 16 * kQkVecThreads<T>)) == cudaSuccess)
     done.fetch_or(bit, std::memory_order_release);
-  k_qk_vec<T, HD><<<dim3(min(a.rows, max(1, most / passes)), passes), threads, smem, s>>>(a);
+  launch_chained(k_qk_vec<T, HD>, dim3(min(a.rows, max(1, most / passes)), passes), dim3(threads), smem, s, a);
 }
 
 template <typename T>
@@ -299,7 +304,7 @@ extern "C" int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream) {
   const int across = (heads + kQkThreads / 32 - 1) / (kQkThreads / 32);
   // few rows: the heads of a row spread over CTAs
   const dim3 grid(min(in->rows, 1 << 20), min(across, max(1, 296 / min(in->rows, 296))));
-  if (in->dtype == DC_F32) k_qk_any<float><<<grid, kQkThreads, 0, s>>>(a);
-  else k_qk_any<__nv_bfloat16><<<grid, kQkThreads, 0, s>>>(a);
+  if (in->dtype == DC_F32) launch_chained(k_qk_any<float>, grid, dim3(kQkThreads), 0, s, a);
+  else launch_chained(k_qk_any<__nv_bfloat16>, grid, dim3(kQkThreads), 0, s, a);
   return op_launched("dc_qk_norm_rope");
 }

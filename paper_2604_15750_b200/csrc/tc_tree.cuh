@@ -332,16 +332,28 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int ctx = a.ctx[b], keys = ctx + R, tile0 = blockIdx.x * a.tiles;
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
   // (a cluster's barriers wait for the CTAs that are still there, and nobody reads the shared memory of one without keys)
-  if (n <= 0 || T <= 0) return;
+  if (n <= 0 || T <= 0) { pdl_wait(); return; }
   uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRingK * C::kSlot;
   TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 96) { ptx::prefetch_tmap(&map_k); ptx::prefetch_tmap(&map_v); }
   if ((ptx::smem_u32(smem_tree) & 1023u) != 0) {   // (it is all the shared memory there is and starts on such a boundary)
+    pdl_wait();
     if (threadIdx.x == 0 && a.status) atomicExch(a.status, DC_ERR_UNSUPPORTED);
     return;
   }
+  if (threadIdx.x == 0) {
+    c.abort_flag = 0; c.late_flag = 0; c.poisoned = 0;
+    for (int i = 0; i < C::kRingK; ++i) { ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1); }
+    for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
+    ptx::mbar_init(&c.p_full, 4 * C::kGroups);       // the softmax warps
+    ptx::mbar_init(&c.p_empty, 1);
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async_smem();
+  }
+  pdl_wait();      // (pdl.cuh: nothing of the caller's memory is read or written before)
 
   // the queries are asked for before the tiles of all CTAs fill the way from memory (by warps 1 ..: warp 0 asks for the tiles)
   constexpr int kAskers = C::kThreads - 32, kItems = (N * 16 + kAskers - 1) / kAskers;
@@ -392,14 +404,6 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     if (!Q8) ptx::tma_load_2d(dst + kSub, &map_v, &c.v_full[s], key + 64, vrow);
   };
   if (threadIdx.x == 0) {
-    c.abort_flag = 0; c.late_flag = 0; c.poisoned = 0;
-    for (int i = 0; i < C::kRingK; ++i) { ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1); }
-    for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
-    ptx::mbar_init(&c.p_full, 4 * C::kGroups);       // the softmax warps
-    ptx::mbar_init(&c.p_empty, 1);
-    ptx::fence_barrier_init();
-    ptx::fence_proxy_async_smem();
     // the first tiles are on their way while the CTA sets up, and only these: the others would be in the way of the queries of the
     // CTAs that start later (8 x 1200 keys, 24 rows: the whole rings 22.6 us, one K tile 21.4, one of each 21.2)
     load_k(0);

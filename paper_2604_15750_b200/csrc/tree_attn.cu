@@ -126,8 +126,7 @@ template <typename T, typename H, int HD>
 bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
   static std::atomic<unsigned long long> done;
   if (!opt_in(k_tree_simt_hd<T, H, HD>, tree_simt_smem_hd(HD), done)) return false;
-  k_tree_simt_hd<T, H, HD><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), 256, tree_simt_smem_hd(HD), s>>>(a);
-  return true;
+  return launch_chained(k_tree_simt_hd<T, H, HD>, dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), dim3(256), tree_simt_smem_hd(HD), s, a) == cudaSuccess;
 }
 
 template <typename T, typename H>
@@ -138,8 +137,7 @@ bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s
   }
   static std::atomic<unsigned long long> done;
   if (!opt_in(k_tree_simt<T, H>, tree_simt_smem(256), done)) return false;
-  k_tree_simt<T, H><<<dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), 128, tree_simt_smem(a.c.head_dim), s>>>(a);
-  return true;
+  return launch_chained(k_tree_simt<T, H>, dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), dim3(128), tree_simt_smem(a.c.head_dim), s, a) == cudaSuccess;
 }
 
 template <int N, bool Q8>
@@ -152,10 +150,12 @@ bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, int v
   if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles); cfg.blockDim = dim3(C::kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = p.joined; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr; cfg.numAttrs = p.cluster ? 1 : 0;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.joined; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = p.cluster ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, k_tree_tc<N, Q8>, mk, mv, a, vec_q, vec_o) == cudaSuccess;
 }
 

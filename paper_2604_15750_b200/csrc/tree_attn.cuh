@@ -122,6 +122,8 @@ __global__ void __launch_bounds__(256, 2) k_tree_simt_hd(const __grid_constant__
   const int b = blockIdx.z / a.line_tiles, R = a.rows[b], G = a.group, nkv = a.c.n_kv_heads;
   const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kSimtLines, n = min(kSimtLines, R * G - line0);
   const int ctx = a.ctx[b], keys = ctx + R, k0 = blockIdx.x * a.tiles * kTreeTile, k1 = min(keys, k0 + a.tiles * kTreeTile);
+  pdl_trigger();
+  pdl_wait();
   if (n <= 0 || k0 >= keys) return;
   float *qs = tree_smem, *ks = qs + kSimtLines * KP, *vs = ks + kSimtKeys * KP, *ps = vs + HD * VP;
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;     // keys 4 tx .. + 3 (dims tx, tx + 16, ..) of lines 2 ty, 2 ty + 1
@@ -291,6 +293,8 @@ __global__ void __launch_bounds__(128) k_tree_simt(const __grid_constant__ TreeA
   const int b = blockIdx.z / a.line_tiles, R = a.rows[b], G = a.group, hd = a.c.head_dim, nkv = a.c.n_kv_heads;
   const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kTreeLines;
   const int keys = a.ctx[b] + R, k0 = blockIdx.x * a.tiles * kTreeTile, k1 = min(keys, k0 + a.tiles * kTreeTile);
+  pdl_trigger();
+  pdl_wait();
   if (line0 >= R * G || k0 >= keys) return;
   float *qs = tree_smem, *ks = qs + kTreeLines * hd, *vs = ks + kTreeKeys * (hd + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
