@@ -168,8 +168,7 @@ __global__ void __launch_bounds__(kTileThreads) k_rows_tile(const __grid_constan
   constexpr int RPT = kTk * LPR / kTileThreads;   // rows a thread: 4 (128), 2 (64)
   const int nkv = a.c.n_kv_heads, b = blockIdx.y / nkv, g = blockIdx.y % nkv, side = blockIdx.z & 1, l = blockIdx.z >> 1;
   const int pos = a.pos[b], end = pos + a.n[b], t0 = (pos / kTk + blockIdx.x) * kTk;
-  pdl_trigger();
-  pdl_wait();
+  pdl_wait();      // (no pdl_trigger: blocks of the next kernel in the places of these cost 5% of a large write)
   if (t0 >= end) return;
   const int lo = max(pos, t0), hi = min(end, t0 + kTk), tid = threadIdx.x;
   const long long* st = side ? a.vs : a.ks;
