@@ -13,6 +13,7 @@ struct RowsArgs {
 };
 
 // ---- any strides, types and alignment: a warp takes one row of K or V -----------------------------------
+// (32 layers of four contexts of up to 1024 keys 6353 us, 13 times k_rows_tile: V goes out value by value)
 // grid (row, sequence * kv head, layer * 2 + side)
 constexpr int kAnyWarps = 8;
 
@@ -70,7 +71,8 @@ __global__ void __launch_bounds__(kAnyWarps * 32) k_rows_any(const RowsArgs a) {
 //   K, either way: 16 (8) lanes a row, 8 dims a lane.
 //   V with contiguous dims: the same, four keys a thread, whose values turn into groups of four keys in shared memory.
 //   V with contiguous keys (ACROSS): 8 keys x 1 dim a lane; a row's maximum comes together over the CTA.
-// Bound by HBM (2 bytes read for 1 written).  Ordinary instructions for a value: one to unpack, one for the maximum (of 16-bit
+// Bound by HBM (2 bytes read for 1 written): 32 layers of four contexts of up to 1024 keys, 2.87 GB, 481 us (6.0 TB/s) with contiguous keys,
+// 594 us with contiguous dims (5.5); 28 layers of four contexts of 768 keys back, 267 MB, 41 us (6.5).  Ordinary instructions for a value: one to unpack, one for the maximum (of 16-bit
 // patterns, two at a time), a half to multiply, a half to convert.
 constexpr int kTk = 64, kTileThreads = 256;
 
