@@ -60,8 +60,9 @@ def tree(q, k, v, ctx, rows, mask, scale):
     return o, p
 
 
-def tree_tolerance(q, k, v, p, o, scale, dtype, vs=None, v8=None, tensor_cores=False):
-    """[rows, hq, hd].  A score z = scale * q.k is off by at most (hd + 4) roundings of the sum of its terms' magnitudes (on the
+def tree_tolerance(q, k, v, p, o, scale, dtype, vs=None, v8=None, tensor_cores=False, outliers=False):
+    """[rows, hq, hd].  outliers: queries against an 8-bit cache are held to 2^-18 of a row's largest value, which counts where other
+    values are 2^10 below it.  A score z = scale * q.k is off by at most (hd + 4) roundings of the sum of its terms' magnitudes (on the
     tensor cores, whose sums drop bits instead of rounding them, twice that), a probability by twice that relative (its own
     score and the sum's), the sum over n keys by n roundings.  On the tensor cores a probability is rounded to 8 bits (2^-8
     at most), and against an 8-bit cache not more finely than 2^-17 of the largest probability x scale of V."""
@@ -74,6 +75,8 @@ def tree_tolerance(q, k, v, p, o, scale, dtype, vs=None, v8=None, tensor_cores=F
         size = (q[:rows, h].double().abs() @ kk.T * scale)
         size = torch.where(p[h] > 0, size, torch.zeros_like(size)).amax(-1, keepdim=True)
         rel = 2 * (2 if tensor_cores else 1) * (hd + 4) * U32 * size * 1.5 + (n + 20) * U32
+        if outliers:
+            rel = rel + 2 * 2.0 ** -18 * q[:rows, h].double().abs().amax(-1, keepdim=True) * kk.sum(-1).amax() * scale
         if tensor_cores:
             rel = rel + 2.0 ** -8
         tol[:, h] = rel * (p[h].nan_to_num(0) @ vv)

@@ -252,6 +252,7 @@ TREES = [  # type of q, held, ctx_len, n_rows, max_rows, hq, hkv, hd, tree
     (BF16, BF16, [127, 129], [17, 40], 40, 8, 8, 128, True), (BF16, E4M3, [2049], [9], 9, 56, 8, 128, True),
     (F32, F32, [64], [16], 16, 4, 4, 64, True), (F32, F32, [1000, 3], [5, 37], 40, 6, 2, 128, True), (F32, E4M3, [300], [20], 20, 4, 1, 64, True),
     (BF16, E4M3, [257], [12], 12, 4, 2, 64, True), (BF16, BF16, [257, 0], [12, 5], 12, 4, 2, 96, True), (F32, F32, [40], [10], 11, 2, 1, 256, False),
+    (F32, F32, [500, 77], [33, 4], 33, 6, 2, 128, True), (F32, E4M3, [190], [70], 70, 3, 1, 128, True), (BF16, BF16, [200], [9], 9, 4, 4, 64, False),
     (F32, F32, [9], [3], 3, 2, 2, 8, True), (BF16, E4M3, [1500], [40], 40, 2, 1, 256, True),
 ]
 
@@ -582,3 +583,24 @@ def test_a_prefilled_context_goes_through_8_bits_into_a_step():
     for n in res[0]:
         assert torch.equal(res[0][n], res[1][n]), n
     eng.close()
+
+
+@pytest.mark.parametrize("far,spread", [(64.0, 0), (3000.0, 30), (1.0, 60)])
+def test_tree_attention_outliers(far, spread):
+    """One channel of the queries far above the others, rows of V whose sizes (and scales) lie 2^spread apart either way."""
+    ctx, rows = [700], [21]
+    c, q, mask, bools = _tree_case(BF16, E4M3, ctx, rows, 21, 4, 2, 128, True)
+    n = 721
+    k = torch.randn((1, n, 2, 128), generator=gen(1))
+    k[..., 5] /= far
+    v = torch.randn((1, n, 2, 128), generator=gen(2)) * torch.exp2(torch.randint(-spread, spread + 1, (1, n, 2, 1), generator=gen(3)).float())
+    dc.cache_write(c, k.to(BF16).to(DEV), v.to(BF16).to(DEV), [0], layer=1)
+    q = q.float()
+    q[..., 5] *= far
+    q = q.to(BF16)
+    out = dc.tree_attention(q.to(DEV), c, ctx, rows, mask.to(DEV), layer=1)
+    kk, v8 = c.k[1, 0].float().cpu() * c.k_scale[1, 0].cpu()[..., None], c.v[1, 0].float().cpu().transpose(1, 2)
+    vs = c.v_scale[1, 0].cpu()
+    vv = v8.double() * vs.double()[..., None]
+    want, p = ref.tree(q[0], kk, vv, 700, 21, bools[0], 128 ** -0.5)
+    near(out[0], want, ref.tree_tolerance(q[0], kk, vv, p, want, 128 ** -0.5, BF16, vs, v8, True, outliers=True))
