@@ -21,6 +21,7 @@ from . import binding as _b
 _TYPES = {torch.float32: _b.DC_F32, torch.bfloat16: _b.DC_BF16, torch.float8_e4m3fn: _b.DC_E4M3}
 _CACHE, _ROWS = Struct("@6i4P"), Struct("@4i2P10q2P")
 _QK, _TREE = Struct("@5i2f2P4q5P4q"), Struct("@5if2P6q4PQP")
+_Tensor, _INT32 = torch.Tensor, torch.int32
 
 
 def _type(t, what):
@@ -32,8 +33,8 @@ def _type(t, what):
 
 def _lengths(values, batch, what):
     """(address, owner) of a host array of `batch` int32: a CPU int32 tensor as it is, anything else copied"""
-    if type(values) is torch.Tensor:
-        if values.dtype == torch.int32 and values.device.type == "cpu" and values.is_contiguous():
+    if type(values) is _Tensor:
+        if values.dtype is _INT32 and not values.is_cuda and values.is_contiguous():
             if values.numel() != batch:
                 raise ValueError(f"{what} has {values.numel()} lengths for {batch} sequences")
             return values.data_ptr(), values
@@ -78,6 +79,18 @@ def _call(f, index, stream, *args):
         raise _b.DepCapError(rc, _b.lib().dc_last_error(None).decode())
 
 
+class _Fn:
+    """The library's functions, looked up once."""
+
+    def __getattr__(self, name):
+        f = getattr(_b.lib(), name)
+        setattr(self, name, f)
+        return f
+
+
+_fn = _Fn()
+
+
 class KvCache:
     """K and V of every layer: k [layers, slots, kv heads, keys, head_dim], v [layers, slots, kv heads, head_dim, keys],
     contiguous, in fp32 or bf16 (then the arrays that `DepCap.step` takes) or in float8_e4m3fn with one fp32 scale per key
@@ -116,13 +129,14 @@ class KvCache:
 
 
 def _move(f, cache, k, v, pos, n, layer, stream):
-    if k.dim() == 4:
-        k = k[None]
+    shape, dtype = k.shape, k.dtype
+    if len(shape) == 4:
+        k, shape = k[None], (1, *shape)
     if v.dim() == 4:
         v = v[None]
-    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype:
-        raise ValueError(f"k {tuple(k.shape)} {k.dtype} and v {tuple(v.shape)} {v.dtype}: [layer,] sequence, row, kv head, dim of one type")
-    layers, batch, most, heads, hd = k.shape
+    if v.shape != shape or v.dtype is not dtype or len(shape) != 5:
+        raise ValueError(f"k {tuple(shape)} {dtype} and v {tuple(v.shape)} {v.dtype}: [layer,] sequence, row, kv head, dim of one type")
+    layers, batch, most, heads, hd = shape
     if heads != cache.n_kv_heads or hd != cache.head_dim:
         raise ValueError(f"rows of {heads} x {hd} with a cache of {cache.n_kv_heads} x {cache.head_dim}")
     index = cache._index
@@ -133,13 +147,13 @@ def _move(f, cache, k, v, pos, n, layer, stream):
     if n is not None and max(n_keep.tolist(), default=0) > most:
         raise ValueError(f"n asks for more than the {most} rows given")
     _call(f, index, stream, cache._c, _ROWS.pack(batch, layer, layers, _type(k, "rows"), k.data_ptr(), v.data_ptr(), *k.stride(),
-                                                  *v.stride(), at, n_at))
+                                                 *v.stride(), at, n_at))
 
 
 def cache_write(cache, k, v, pos, n=None, layer=0, stream=None):
     """dc_cache_write: rows k, v [layers, sequences, rows, kv heads, head_dim] (or without the layers: one) become keys
     pos[b] .. pos[b] + n[b] - 1 of slot b in the cache's layers from `layer` on.  Any strides; n: all rows."""
-    _move(_b.lib().dc_cache_write, cache, k, v, pos, n, layer, stream)
+    _move(_fn.dc_cache_write, cache, k, v, pos, n, layer, stream)
     return cache
 
 
@@ -147,7 +161,7 @@ def cache_read(cache, k, v, pos, n=None, layer=0, stream=None):
     """dc_cache_read: the other way round, into k and v; rows >= n[b] are left as they were."""
     _apart(k.shape, k.stride(), "k")
     _apart(v.shape, v.stride(), "v")
-    _move(_b.lib().dc_cache_read, cache, k, v, pos, n, layer, stream)
+    _move(_fn.dc_cache_read, cache, k, v, pos, n, layer, stream)
     return k, v
 
 
@@ -156,25 +170,23 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
     int32 [rows] on the device, gains [head_dim] of q's type (None: 1).  Returns q_out, k_out (new ones where None; they may
     be q and k themselves)."""
     dtype, index, shape, kshape = q.dtype, q.get_device(), q.shape, k.shape
-    if len(shape) != 3 or len(kshape) != 3 or shape[0] != kshape[0] or shape[2] != kshape[2] or k.dtype != dtype:
+    if len(shape) != 3 or len(kshape) != 3 or shape[0] != kshape[0] or shape[2] != kshape[2] or k.dtype is not dtype:
         raise ValueError(f"q {tuple(shape)} {dtype}, k {tuple(kshape)} {k.dtype}: [rows, heads, head_dim] of one type")
     rows, hq, hd = shape
     if q_out is None:
         q_out = torch.empty(shape, dtype=dtype, device=q.device)
     if k_out is None:
         k_out = torch.empty(kshape, dtype=dtype, device=q.device)
-    if q_out.shape != shape or k_out.shape != kshape or q_out.dtype != dtype or k_out.dtype != dtype:
+    if q_out.shape != shape or k_out.shape != kshape or q_out.dtype is not dtype or k_out.dtype is not dtype:
         raise ValueError("an output has another shape or type than its input")
-    if pos.dtype != torch.int32 or pos.dim() != 1 or pos.numel() != rows or not pos.is_contiguous():
+    if pos.dtype is not _INT32 or pos.dim() != 1 or pos.numel() != rows or not pos.is_contiguous():
         raise ValueError(f"pos is a contiguous int32 tensor of {rows} positions")
-    gains = []
-    for g in (q_gain, k_gain):
-        if g is None:
-            gains.append(0)
-            continue
-        if g.dtype != dtype or g.dim() != 1 or g.numel() != hd or not g.is_contiguous() or g.get_device() != index:
-            raise ValueError(f"a gain is a contiguous tensor of {hd} values of {dtype} on {q.device}")
-        gains.append(g.data_ptr())
+    gain_at = [0, 0]
+    for i, g in enumerate((q_gain, k_gain)):
+        if g is not None:
+            if g.dtype is not dtype or g.shape != (hd,) or not g.is_contiguous() or g.get_device() != index:
+                raise ValueError(f"a gain is a contiguous tensor of {hd} values of {dtype} on {q.device}")
+            gain_at[i] = g.data_ptr()
     if not k.get_device() == pos.get_device() == q_out.get_device() == k_out.get_device() == index:
         _elsewhere(q.device, k, pos, q_out, k_out)
     a, b, d = q.stride()
@@ -182,13 +194,14 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
     qo, ko = q_out.stride(), k_out.stride()
     if hd > 1 and not d == h == qo[2] == ko[2] == 1:
         raise ValueError("the dims of a head are contiguous")
-    _apart(shape, qo, "q_out")
-    _apart(kshape, ko, "k_out")
+    if 0 in qo or 0 in ko:
+        _apart(shape, qo, "q_out")
+        _apart(kshape, ko, "k_out")
     x, y, u, w = q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()
     if (x == u and x and qo != (a, b, d)) or (y == w and y and ko != (e, f, h)):
         raise ValueError("an output in the place of its input has the same strides")
-    _call(_b.lib().dc_qk_norm_rope, index, stream,
-          _QK.pack(_type(q, "q"), rows, hq, kshape[1], hd, eps, rope_theta, x, y, a, b, e, f, *gains, pos.data_ptr(), u, w, qo[0], qo[1],
+    _call(_fn.dc_qk_norm_rope, index, stream,
+          _QK.pack(_type(q, "q"), rows, hq, kshape[1], hd, eps, rope_theta, x, y, a, b, e, f, *gain_at, pos.data_ptr(), u, w, qo[0], qo[1],
                    ko[0], ko[1]))
     return q_out, k_out
 
@@ -210,7 +223,8 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
     os_ = out.stride()
     if d != 1 or os_[3] != 1:
         raise ValueError("the dims of a head are contiguous")
-    _apart(shape, os_, "out")
+    if 0 in os_:
+        _apart(shape, os_, "out")
     mask_at = 0
     if mask is not None:
         if mask.dtype not in (torch.int32, torch.uint32) or mask.shape != (batch, rows, (rows + 31) // 32) or not mask.is_contiguous():
@@ -229,7 +243,7 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
     n, n_keep = _lengths(n_rows, batch, "n_rows")
     args = (batch, layer, _type(q, "q"), heads, rows, scale, q.data_ptr(), out.data_ptr(), a, b, h, os_[0], os_[1], os_[2], ctx, n, mask_at)
     st = 0 if status is None else status.data_ptr()
-    call = _b.lib().dc_tree_attention
+    call = _fn.dc_tree_attention
     if workspace is None:
         # most calls want none: whether this one does is asked only after a refusal, which launches nothing
         try:
@@ -248,7 +262,7 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
 
 def _need(cache, packed):
     need = C.c_uint64()
-    _call(lambda c, a, stream: _b.lib().dc_tree_attention_workspace(c, a, C.addressof(need)), cache._index, None, cache._c, packed)
+    _call(lambda c, a, stream: _fn.dc_tree_attention_workspace(c, a, C.addressof(need)), cache._index, None, cache._c, packed)
     return need.value
 
 
