@@ -290,7 +290,8 @@ extern "C" int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream) {
   if (!in->pos || (in->n_q_heads && (!in->q || !in->q_out)) || (in->n_kv_heads && (!in->k || !in->k_out)))
     return op_fail(DC_ERR_INVALID_ARG, "null argument");
   QkArgs a;
-  a.x[0] = in->q; a.x[1] = in->k; a.gain[0] = in->q_gain; a.gain[1] = in->k_gain; a.y[0] = in->q_out; a.y[1] = in->k_out;
+  a.x[0] = in->q; a.x[1] = in->k; a.y[0] = in->q_out; a.y[1] = in->k_out;
+  a.gain[0] = in->n_q_heads ? in->q_gain : nullptr; a.gain[1] = in->n_kv_heads ? in->k_gain : nullptr;   // (not looked at without heads)
   for (int i = 0; i < 2; ++i) {
     a.xs[0][i] = in->q_stride[i]; a.xs[1][i] = in->k_stride[i];
     a.ys[0][i] = in->q_out_stride[i]; a.ys[1][i] = in->k_out_stride[i];

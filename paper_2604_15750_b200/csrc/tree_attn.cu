@@ -103,6 +103,8 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   if (in->layer < 0 || in->layer >= c->n_layers) return op_fail(DC_ERR_SHAPE, "layer %d of %d", in->layer, c->n_layers);
   if (in->n_q_heads < 1 || in->n_q_heads % c->n_kv_heads)
     return op_fail(DC_ERR_INVALID_ARG, "%d query heads over %d kv heads", in->n_q_heads, c->n_kv_heads);
+  if (in->n_q_heads / c->n_kv_heads > kTreeMaxGroup)     // (tree_row)
+    return op_fail(DC_ERR_UNSUPPORTED, "more than %d query heads of a kv head", kTreeMaxGroup);
   if (in->max_rows < 1 || in->max_rows > DC_MAX_WINDOW) return op_fail(DC_ERR_SHAPE, "max_rows=%d outside [1, %d]", in->max_rows, (int)DC_MAX_WINDOW);
   if (!(in->scale >= 0.f) || in->scale > 1e30f) return op_fail(DC_ERR_INVALID_ARG, "scale outside [0, 1e30]");
   if ((rc = op_check_keys(c, in->batch, in->ctx_len, in->n_rows, in->max_rows, ", max_rows bounds the rows")) != DC_OK) return rc;

@@ -37,7 +37,8 @@ __device__ __forceinline__ int tree_stretches(const TreeArgs& a, int b) {
   const int t = (a.ctx[b] + a.rows[b] + kTreeTile - 1) / kTreeTile;
   return (t + a.tiles - 1) / a.tiles;
 }
-// row of line m: m / group, exactly where m * group < 2^32 (a sequence has 2^19 lines at most, a group 2^11)
+// row of line m: m / group, exactly where m * group < 2^32: a sequence has 2^19 lines at most
+constexpr int kTreeMaxGroup = 2048;
 __device__ __forceinline__ int tree_row(const TreeArgs& a, int m) { return a.group == 1 ? m : (int)__umulhi((uint32_t)m, a.group_inv); }
 // place of (sequence, row, query head) among the lines
 __device__ __forceinline__ int tree_line(const TreeArgs& a, int b, int r, int h) { return a.base[b] + r * a.nq + h; }
@@ -357,6 +358,7 @@ __global__ void __launch_bounds__(128) k_tree_simt(const __grid_constant__ TreeA
       if (__any_sync(0xffffffffu, sees)) {     // (a NaN score makes the row NaN, whatever the maximum is)
         const float f = top[j] == -INFINITY ? 0.f : exp2f(top[j] - now);
         p = sees ? exp2f(z[j] - now) : 0.f;
+        if (sees && p == 0.f) p = 1.4e-45f;    // (below all others, but V's infinities and NaN of a key that is seen arrive)
         l[j] = l[j] * f + p;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[j][i] *= f;

@@ -79,6 +79,14 @@ def _call(f, index, stream, *args):
         raise _b.DepCapError(rc, _b.lib().dc_last_error(None).decode())
 
 
+_HERE = nullcontext()
+
+
+def _on(stream):
+    """What is allocated (and filled) for a call belongs to the stream that its work goes to."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
 class _Fn:
     """The library's functions, looked up once."""
 
@@ -173,10 +181,10 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
     if len(shape) != 3 or len(kshape) != 3 or shape[0] != kshape[0] or shape[2] != kshape[2] or k.dtype is not dtype:
         raise ValueError(f"q {tuple(shape)} {dtype}, k {tuple(kshape)} {k.dtype}: [rows, heads, head_dim] of one type")
     rows, hq, hd = shape
-    if q_out is None:
-        q_out = torch.empty(shape, dtype=dtype, device=q.device)
-    if k_out is None:
-        k_out = torch.empty(kshape, dtype=dtype, device=q.device)
+    if q_out is None or k_out is None:
+        with _on(stream):
+            q_out = torch.empty(shape, dtype=dtype, device=q.device) if q_out is None else q_out
+            k_out = torch.empty(kshape, dtype=dtype, device=q.device) if k_out is None else k_out
     if q_out.shape != shape or k_out.shape != kshape or q_out.dtype is not dtype or k_out.dtype is not dtype:
         raise ValueError("an output has another shape or type than its input")
     if pos.dtype is not _INT32 or pos.dim() != 1 or pos.numel() != rows or not pos.is_contiguous():
@@ -216,7 +224,8 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         raise ValueError(f"q {tuple(shape)}: sequences, rows, heads, head_dim={cache.head_dim}")
     batch, rows, heads, hd = shape
     if out is None:
-        out = torch.zeros(shape, dtype=dtype, device=q.device)
+        with _on(stream):
+            out = torch.zeros(shape, dtype=dtype, device=q.device)
     elif out.shape != shape or out.dtype != dtype:
         raise ValueError("out has another shape or type than q")
     a, b, h, d = q.stride()
@@ -232,6 +241,8 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         mask_at = mask.data_ptr()
     if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
         raise ValueError("status is one int32")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace is contiguous")
     if scale is None:
         scale = 0.0
     elif not scale > 0:
@@ -253,8 +264,7 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
             size = _need(cache, _TREE.pack(*args, 0, 0, st))
             if not size:
                 raise
-        # (of the stream that the work goes to, so that the allocator hands it out again in that order)
-        with nullcontext() if stream is None else torch.cuda.stream(stream):
+        with _on(stream):
             workspace = torch.empty(size, dtype=torch.uint8, device=cache.device)
     _call(call, index, stream, cache._c, _TREE.pack(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), st))
     return out

@@ -381,6 +381,25 @@ def test_tree_attention_values_that_are_not_finite_stay_with_the_rows_that_see_t
     assert bools[0, :, j].any() and not bools[0, :, j].all()
 
 
+@pytest.mark.parametrize("held,hd", [(E4M3, 128), (BF16, 128), (BF16, 64), (BF16, 96), (E4M3, 8)])
+def test_tree_attention_a_value_that_is_not_finite_behind_a_probability_of_zero(held, hd):
+    """A drafted key far below the others' scores: rows that see it are NaN where its V is, the others as they were."""
+    c, q, mask, bools = _tree_case(BF16, held, [100], [40], 40, 4, 2, hd, True)
+    q = torch.full_like(q, 4.0)
+    key, value = torch.full((1, 1, 2, hd), -64.0, dtype=BF16), torch.ones((1, 1, 2, hd), dtype=BF16)
+    dc.cache_write(c, key.to(DEV), value.to(DEV), [105], layer=1)
+    before = dc.tree_attention(q.to(DEV), c, [100], [40], mask.to(DEV), layer=1).cpu()
+    value[..., 3] = math.nan
+    dc.cache_write(c, key.to(DEV), value.to(DEV), [105], layer=1)
+    out = dc.tree_attention(q.to(DEV), c, [100], [40], mask.to(DEV), layer=1).cpu()
+    assert not torch.isnan(before).any() and bools[0, :, 5].any()
+    for r in range(40):
+        if bools[0, r, 5]:
+            assert torch.isnan(out[0, r, :, 3]).all()
+        else:
+            assert torch.equal(out[0, r], before[0, r])
+
+
 @pytest.mark.parametrize("held,hd", [(E4M3, 128), (BF16, 128), (F32, 64)])
 def test_tree_attention_strides_and_bases(held, hd):
     """q and out as slices of larger tensors, out head by head; arrays off 16-byte boundaries."""
@@ -455,7 +474,9 @@ def test_calls_on_other_streams_in_graphs_and_twice(held):
     assert torch.equal(first, dc.tree_attention(qd, c, ctx, rows, md, layer=1))
     torch.cuda.synchronize()
     side = [torch.cuda.Stream() for _ in range(2)]
-    outs = [dc.tree_attention(qd, c, ctx, rows, md, layer=1, stream=s, out=torch.zeros_like(qd)) for s in side]
+    outs = [torch.zeros_like(qd) for _ in side]
+    torch.cuda.synchronize()
+    outs = [dc.tree_attention(qd, c, ctx, rows, md, layer=1, stream=s, out=o) for s, o in zip(side, outs)]
     torch.cuda.synchronize()
     assert all(torch.equal(o, first) for o in outs)
     pos = torch.arange(48, dtype=torch.int32, device=DEV)
@@ -476,6 +497,21 @@ def test_calls_on_other_streams_in_graphs_and_twice(held):
         dc.cache_write(c, kv, kv, ctx, rows, layer=1)
         assert torch.equal(got, dc.tree_attention(qn.view(2, 24, 8, 128), c, ctx, rows, md, layer=1))
         _check_tree(c, 1, qn.view(2, 24, 8, 128), ctx, rows, bools, got)
+
+
+def test_outputs_made_for_a_call_on_another_stream_belong_to_that_stream():
+    """The current stream is busy when the call is made: nothing of the output may wait for it."""
+    c, q, mask, _ = _tree_case(BF16, E4M3, [200], [24], 24, 8, 4, 128, True)
+    qd, md = q.to(DEV), mask.to(DEV)
+    h, pos = qd[0], torch.arange(24, dtype=torch.int32, device=DEV)
+    want, turned = dc.tree_attention(qd, c, [200], [24], md, layer=1), dc.qk_norm_rope(h, h, pos)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda._sleep(20_000_000)        # (10 ms)
+        got, (a, b) = dc.tree_attention(qd, c, [200], [24], md, layer=1, stream=side), dc.qk_norm_rope(h, h, pos, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(a, turned[0]) and torch.equal(b, turned[1])
 
 
 def test_a_workspace_of_the_callers_own():

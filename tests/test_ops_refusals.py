@@ -96,7 +96,8 @@ def test_null_arguments_and_nothing_to_do():
 
 @pytest.mark.parametrize("bad,code", [
     (dict(dtype=b.DC_E4M3), INVALID), (dict(batch=0), SHAPE), (dict(batch=5), SHAPE), (dict(layer=2), SHAPE), (dict(layer=-1), SHAPE),
-    (dict(n_q_heads=3), INVALID), (dict(n_q_heads=0), INVALID), (dict(max_rows=0), SHAPE), (dict(max_rows=257), SHAPE),
+    (dict(n_q_heads=3), INVALID), (dict(n_q_heads=0), INVALID), (dict(n_q_heads=4098, n_rows=ints(1, 0)), UNSUPPORTED),
+    (dict(n_q_heads=1 << 18, max_rows=1, n_rows=ints(1, 0)), UNSUPPORTED), (dict(max_rows=0), SHAPE), (dict(max_rows=257), SHAPE),
     (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=1e31), INVALID), (dict(ctx_len=None), INVALID),
     (dict(n_rows=None), INVALID), (dict(ctx_len=ints(-1, 0)), SHAPE), (dict(n_rows=ints(0, 17)), SHAPE), (dict(n_rows=ints(-1, 1)), SHAPE),
     (dict(ctx_len=ints(120, 0), n_rows=ints(9, 0)), SHAPE), (dict(ctx_len=ints(2 ** 31 - 1, 0), n_rows=ints(16, 0)), SHAPE),
@@ -191,7 +192,8 @@ def test_the_binding_refuses():
     with pytest.raises(RuntimeError, match="no CPU path"):
         dc.tree_attention(q, c, [0, 0], [3, 3])
     for kw in [dict(mask=torch.zeros((2, 3, 2), dtype=torch.int32)), dict(mask=torch.zeros((2, 3, 1))), dict(out=q[:, :2]), dict(out=q.float()),
-               dict(scale=0.0), dict(scale=-1.0), dict(status=torch.zeros(2, dtype=torch.int32)), dict(out=q[:, :1].expand(2, 3, 4, 128))]:
+               dict(scale=0.0), dict(scale=-1.0), dict(status=torch.zeros(2, dtype=torch.int32)),
+               dict(workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 20)), dict(out=q[:, :1].expand(2, 3, 4, 128))]:
         with pytest.raises(ValueError):
             dc.tree_attention(q, c, [0, 0], [3, 3], **kw)
     for bad in [(q[..., :64], c, [0, 0], [3, 3]), (q[0], c, [0, 0], [3, 3]), (q, c, [0], [3, 3]), (q.transpose(2, 3).contiguous().transpose(2, 3), c, [0, 0], [3, 3])]:
