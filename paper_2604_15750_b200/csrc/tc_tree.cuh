@@ -33,8 +33,8 @@
 //
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
-// would be NaN for lines that do not see the key), 4 .. = softmax and output, four warps for every 16 lines, or 32 of 128 (warp 3
-// has nothing to do: a warp reads the quarter of TMEM's lanes that its number says).
+// would be NaN for lines that do not see the key), 3 = factors that the scales of e4m3 keys make, 4 .. = softmax and output, four
+// warps for every 16 lines, or 32 of 128 (a warp reads the quarter of TMEM's lanes that its number says).
 #pragma once
 #include "tc_attn_parts.cuh"
 #include "tree_attn.cuh"
@@ -47,12 +47,13 @@ struct TreeTc {
   static constexpr int kGroups = N / kLines, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
   // slots of the rings, as shared memory has room
-  static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : (Q8 ? 4 : 2);
+  static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : (Q8 ? 3 : 2);
+  static constexpr int kP = Q8 && N >= 64 ? 2 : 1;             // tiles of P: with two no warp waits for the product before
   static constexpr int kRingV = N == 32 ? 3 : kRingK;
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
-  static constexpr int kCtl = (N == 128 ? 8 : 3) * 1024;
-  static constexpr int kSmem = 2 * kOperand + (kRingK + kRingV) * kSlot + kCtl;
+  static constexpr int kCtl = ((N == 128 ? 5 : 3) + (Q8 ? 4 : 0)) * 1024;
+  static constexpr int kSmem = (1 + kP) * kOperand + (kRingK + kRingV) * kSlot + kCtl;
   // P: the rows of the keys, of 128 bytes at most; a second half of the lines lies behind (bf16, 128 lines)
   static constexpr int kPRow = Q8 ? N : N == 128 ? 128 : 2 * N;
   static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : N == 64 ? 256 : 512;   // TMEM: S^T twice, O^T (its two parts)
@@ -62,9 +63,9 @@ struct TreeTc {
 // m moves costs about half a tile.
 constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.8f, kAhead = 1.f;
 
-template <int N>
+template <int N, bool Q8>
 struct TreeCtl {
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full, p_empty;
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full[2], p_empty[2];
   uint32_t tmem_base;
   int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
@@ -73,6 +74,7 @@ struct TreeCtl {
   long long at[N];                       // places of the lines in o or part_o
   alignas(16) float rs[N];               // e4m3: 2^e of a line's q
   alignas(16) float part[4][N];
+  float4 key[2][Q8 ? kTreeTile : 1];     // e4m3: factor of a key's scores, log2 of V's scale, factor of the sums
 };
 
 // Sum of v[col] over the lanes of a warp, 16 columns at once: lane i returns that of column i % 16.
@@ -342,9 +344,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
   // (a cluster's barriers wait for the CTAs that are still there, and nobody reads the shared memory of one without keys)
   if (n <= 0 || T <= 0) { pdl_wait(); return; }
-  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kOperand, *vring = kring + C::kRingK * C::kSlot;
-  TreeCtl<N>& c = *reinterpret_cast<TreeCtl<N>*>(vring + C::kRingV * C::kSlot);
-  static_assert(sizeof(TreeCtl<N>) <= C::kCtl, "control block");
+  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kP * C::kOperand, *vring = kring + C::kRingK * C::kSlot;
+  TreeCtl<N, Q8>& c = *reinterpret_cast<TreeCtl<N, Q8>*>(vring + C::kRingV * C::kSlot);
+  static_assert(sizeof(TreeCtl<N, Q8>) <= C::kCtl, "control block");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 96) { ptx::prefetch_tmap(&map_k); ptx::prefetch_tmap(&map_v); }
   if ((ptx::smem_u32(smem_tree) & 1023u) != 0) {   // (it is all the shared memory there is and starts on such a boundary)
@@ -356,9 +358,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     c.abort_flag = 0; c.late_flag = 0; c.poisoned = 0;
     for (int i = 0; i < C::kRingK; ++i) { ptx::mbar_init(&c.k_full[i], 1); ptx::mbar_init(&c.k_empty[i], 1); }
     for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
-    ptx::mbar_init(&c.p_full, 4 * C::kGroups);       // the softmax warps
-    ptx::mbar_init(&c.p_empty, 1);
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], Q8 ? 2 : 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
+    for (int i = 0; i < C::kP; ++i) { ptx::mbar_init(&c.p_full[i], 4 * C::kGroups); ptx::mbar_init(&c.p_empty[i], 1); }   // (full: the softmax warps)
     ptx::fence_barrier_init();
     ptx::fence_proxy_async_smem();
   }
@@ -373,20 +374,23 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     if (warp > 0 && item < N * 16) tree_load_q<N, Q8>(a, b, g, line0, n, vec_q, item, q[i]);
   }
   // softmax warps: who sees this thread's key, a bit for each of the warp's lines: tiles without drafted keys by the keys' number
-  // alone, the (at most three) others by the mask; and the scales of this thread's key in the tile to come
+  // alone, the (at most three) others by the mask
   const int draft0 = ctx / kTreeTile;
   uint32_t seen[3], of_line[3];
-  float ks = 0.f, vs = 1.f;
-  const float* k_scale = nullptr;
-  const float* v_scale = nullptr;
+  float ks[4], vs[4];     // warp 3: the scales of keys lane, lane + 32, .. of a tile
+  const size_t scales = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + lane;
+  auto load_scales = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool there = (tile0 + j) * kTreeTile + 32 * i + lane < keys;
+      ks[i] = there ? a.c.k_scale[scales + (size_t)j * kTreeTile + 32 * i] : 0.f;
+      vs[i] = there ? a.c.v_scale[scales + (size_t)j * kTreeTile + 32 * i] : 1.f;
+    }
+  };
+  if (Q8 && warp == 3) load_scales(0);
   if (warp >= 4) {
     const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * C::kLines, line = line0 + col0 + lane % C::kLines;
     const uint32_t* row = a.mask && line < line0 + n ? a.mask + ((size_t)b * a.max_rows + tree_row(a, line)) * a.words : nullptr;
-    if (Q8) {
-      const size_t at = (size_t)(b * nkv + g) * a.c.max_ctx + (size_t)tile0 * kTreeTile + quarter * 32 + lane;
-      k_scale = a.c.k_scale + at; v_scale = a.c.v_scale + at;
-      if (tile0 * kTreeTile + quarter * 32 + lane < keys) { ks = *k_scale; vs = *v_scale; }
-    }
 #pragma unroll
     for (int i = 0; i < 3; ++i) {      // lane = line: the 32 keys of the warp's quarter
       const int jd = (draft0 + i) * kTreeTile + quarter * 32 - ctx, w = jd >> 5;
@@ -495,7 +499,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           ptx::fence_proxy_async_smem();
           __syncwarp();
         }
-        ok = tree_wait_warp(&c.p_full, (uint32_t)j & 1u, abort_flag);
+        ok = tree_wait_warp(&c.p_full[j % C::kP], (uint32_t)(j / C::kP) & 1u, abort_flag);
       } else {
         if (j >= 2) ok = tree_wait_warp(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag);
         ok = ok && tree_wait_warp(&c.k_full[s], (uint32_t)(j / C::kRingK) & 1u, abort_flag);
@@ -512,7 +516,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= nk) break;
-              tree_umma<Q8>(pv ? d + part * N : d, t + kk * 2, a_hi, b_lo + part * b_half + kk * b_step, b_hi, idesc,
+              tree_umma<Q8>(pv ? d + part * N : d, t + kk * 2, a_hi, b_lo + (pv && j % C::kP ? C::kOperand >> 4 : 0) + part * b_half + kk * b_step, b_hi, idesc,
                             (kk > 0 || (pv ? j > 0 : part > 0)) ? 1u : 0u);
             }
         } else {
@@ -524,9 +528,26 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           }
         }
         ptx::umma_commit(pv ? &c.v_empty[s] : &c.k_empty[s]);
-        ptx::umma_commit(pv ? &c.p_empty : &c.s_full[j & 1]);
+        ptx::umma_commit(pv ? &c.p_empty[j % C::kP] : &c.s_full[j & 1]);
       }
       __syncwarp();
+    }
+  } else if (Q8 && warp == 3) {
+    // ---------------- factors of the keys, two tiles ahead of the softmax: each once and not by every group of warps, and the
+    // scales' way from memory is nobody's wait ----------------
+    for (int j = 0; j < T; ++j) {
+      float4 f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v_sc = vs[i] < 7.8886091e-31f ? 7.8886091e-31f : vs[i];   // 2^-100 (a row of zeros may come with a scale of 0: it counts in the sum)
+        f[i] = make_float4(ks[i] * a.scale_log2, tree_lg2(v_sc), v_sc <= 3.402823466e38f ? tree_rcp(v_sc * 16.f) : 0.f, 0.f);
+      }
+      if (j + 1 < T) load_scales(j + 1);
+      if (j >= 2 && !tree_wait_warp(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag)) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.key[j & 1][32 * i + lane] = f[i];
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&c.s_full[j & 1]);
     }
   } else if (warp >= 4) {
     // ---------------- softmax: one thread per key of the tile, 16 lines ----------------
@@ -571,18 +592,12 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int j = 0; j < T; ++j) {
       const int tile = tile0 + j, d = tile - draft0;
       const uint32_t sees = d < 0 ? 0xffffffffu : d == 0 ? seen[0] : d == 1 ? seen[1] : seen[2];
-      const float mul = Q8 ? ks * a.scale_log2 : a.scale_log2;
-      // (a row of zeros may come with a scale of 0: it counts in the sum)
-      const float v_sc = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;   // 2^-100
-      const float lv = Q8 ? tree_lg2(v_sc) : 0.f, iv = Q8 && v_sc <= 3.402823466e38f ? tree_rcp(v_sc * 16.f) : 0.f;
-      if (Q8) {
-        k_scale += kTreeTile; v_scale += kTreeTile;
-        if (j + 1 < T && key < valid_keys(j + 1)) { ks = *k_scale; vs = *v_scale; }
-      }
       ok = ok && tree_wait_warp(&c.s_full[j & 1], ((uint32_t)j >> 1) & 1u, abort_flag);
       // (whatever their waits said, the four warps of a group come to its barriers together: a wait that ran out is a no in the
       // vote on the maxima, and the vote behind it ends the loop for all four)
       ptx::tc_fence_after();
+      const float4 of_key = Q8 ? c.key[j & 1][key] : make_float4(a.scale_log2, 0.f, 0.f, 0.f);
+      const float mul = of_key.x, lv = of_key.y, iv = of_key.z;
       const uint32_t s_col = t_lane + (uint32_t)(j & 1) * N;
       float v[QN][16];
       auto scores = [&]() {
@@ -618,7 +633,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           if (lane == 0) *reinterpret_cast<float4*>(&c.part[quarter][col0 + i]) = make_float4(u[0], u[1], u[2], u[3]);
         }
         if (j > 0)   // O^T: all products so far are in
-          ok = ok && tree_wait_warp(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag);
+          ok = ok && tree_wait_warp(&c.p_empty[(j - 1) % C::kP], (uint32_t)((j - 1) / C::kP) & 1u, abort_flag);
         ok = ptx::all_agree(bar, 128, ok);
         if (!ok) break;
         if (quarter == 0 && lane < CW) {
@@ -651,14 +666,28 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.s_empty[j & 1]);
-      uint32_t hi[QN][8], lo[QN][4];     // bf16: 16 lines; e4m3: 16 lines of each part
+      auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+      };
+      uint32_t hi[QN][Q8 ? 4 : 8], lo[QN][Q8 ? 4 : 1];     // bf16: 16 lines; e4m3: 16 lines of each part
+      const uint32_t p_at = C::kP == 2 && (j & 1) ? (uint32_t)C::kOperand : 0u;
+      auto store = [&](int q, const auto& h, const auto& l) {
+        st16(p_piece(q, 0) + p_at, h[0], h[1], h[2], h[3]);
+        if constexpr (Q8) st16(p_piece(q, 0) + p_at + 128 * C::kPRow, l[0], l[1], l[2], l[3]);
+        else st16(p_piece(q, 1) + p_at, h[4], h[5], h[6], h[7]);
+      };
+      // the P before in this place has been read (a warp whose wait ran out goes on to the next barrier of its group)
+      if (C::kP == 2) {
+        if (j > 1) ok = tree_wait_warp(&c.p_empty[j & 1], (uint32_t)((j - 2) >> 1) & 1u, abort_flag);
+        if (!ok) continue;
+      }
       const ptx::f32x2 iv2 = ptx::f2_pack(iv, iv);
 #pragma unroll
-      for (int q = 0; q < QN; ++q)
+      for (int q = 0; q < QN; ++q) {
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const float p0 = attn_ex2(v[q][i]), p1 = attn_ex2(v[q][i + 1]), p2 = attn_ex2(v[q][i + 2]), p3 = attn_ex2(v[q][i + 3]);
-          if (!Q8) {
+          if constexpr (!Q8) {
             acc[q][i / 2] = ptx::f2_add(acc[q][i / 2], ptx::f2_pack(p0, p1));
             acc[q][i / 2 + 1] = ptx::f2_add(acc[q][i / 2 + 1], ptx::f2_pack(p2, p3));
             const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
@@ -670,24 +699,20 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
             tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[q][i / 4], lo[q][i / 4]);
           }
         }
-      // P of the tile before has been read (a warp whose wait ran out goes on to the next barrier of its group)
-      if (j > 0) ok = tree_wait_warp(&c.p_empty, (uint32_t)(j - 1) & 1u, abort_flag);
-      if (!ok) continue;
-      auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-      };
+        if (C::kP == 2) store(q, hi[q], lo[q]);
+      }
+      if (C::kP == 1) {
+        if (j > 0) ok = tree_wait_warp(&c.p_empty[0], (uint32_t)(j - 1) & 1u, abort_flag);
+        if (!ok) continue;
 #pragma unroll
-      for (int q = 0; q < QN; ++q) {
-        st16(p_piece(q, 0), hi[q][0], hi[q][1], hi[q][2], hi[q][3]);
-        if (Q8) st16(p_piece(q, 0) + 128 * C::kPRow, lo[q][0], lo[q][1], lo[q][2], lo[q][3]);
-        else st16(p_piece(q, 1), hi[q][4], hi[q][5], hi[q][6], hi[q][7]);
+        for (int q = 0; q < QN; ++q) store(q, hi[q], lo[q]);
       }
       ptx::fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&c.p_full);
+      if (lane == 0) ptx::mbar_arrive(&c.p_full[j % C::kP]);
     }
     // O^T is complete once the last P has been read
-    if (ok) ok = tree_wait_warp(&c.p_empty, (uint32_t)(T - 1) & 1u, abort_flag);
+    if (ok) ok = tree_wait_warp(&c.p_empty[(T - 1) % C::kP], (uint32_t)((T - 1) / C::kP) & 1u, abort_flag);
 #pragma unroll
     for (int q = 0; q < QN; ++q) {
       float sum[16];
