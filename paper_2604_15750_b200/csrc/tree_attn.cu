@@ -20,48 +20,126 @@ int sm_count() {
   return v;
 }
 
+// once per device and kernel: shared memory beyond 48 KB
+template <typename K>
+bool opt_in(K kernel, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (done.load(std::memory_order_acquire) & bit) return true;
+  // (two CTAs on an SM, in clusters too, want all of its shared memory)
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_release);
+  return true;
+}
+template <int N, bool Q8>
+bool opt_in_tc() {
+  static std::atomic<unsigned long long> done;
+  return opt_in(k_tree_tc<N, Q8>, TreeTc<N, Q8>::kSmem, done);
+}
+
+// CTAs of k_tree_tc that run at once in clusters of `size`: an SM without enough free neighbours in its part of the device
+// gets none (a property of the device)
+constexpr int kMaxCluster = 8;
+template <int N, bool Q8>
+int cluster_slots(int size) {
+  using C = TreeTc<N, Q8>;
+  static std::atomic<int> known[64][kMaxCluster + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); dev = 64; }
+  int v = dev < 64 ? known[dev][size].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(size); cfg.blockDim = dim3(C::kThreads); cfg.dynamicSmemBytes = C::kSmem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = size; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    if (!opt_in_tc<N, Q8>() || cudaOccupancyMaxActiveClusters(&v, k_tree_tc<N, Q8>, &cfg) != cudaSuccess || v < 1) {
+      cudaGetLastError();
+      v = sm_count() / size;
+    }
+    // (it counts one CTA an SM; where two have room, they do run: 256 CTAs of pairs took one round)
+    v = v < 1 ? size : v * size * C::kResident;
+    if (dev < 64) known[dev][size].store(v, std::memory_order_relaxed);
+  }
+  return v;
+}
+
 // Units of one call: stretches of `tiles` tiles of keys, `line_tiles` stretches of lines a sequence.
 struct TreePlan {
-  int lines_per_unit, slots;
+  int shape;                 // lines of a unit
+  bool tc;
   int tiles, joined, line_tiles, cluster;
   int lines, base[DC_MAX_BATCH];
   uint64_t bytes;
+  long long cost;
 };
 
-// The stretch that ends first when `slots` units run at once: a unit costs its tiles and a start (barriers, queries, the first
-// loads' latency, the output), joining costs a cluster's barriers or a launch; all in the time of a tile.
-constexpr int kUnitStart = 4, kJoinCluster = 1, kJoinLaunch = 4;
-constexpr int kMaxCluster = 8;
+// What units of one kernel take, in 10 ns, measured where K and V come from L2: a tile of 128 keys and the rest of a unit (barriers,
+// queries, the first loads' way, the output), with every place of the SMs taken and with one unit an SM; and what it takes more as a
+// CTA of a cluster
+struct TreeCost { int lines, resident, tile, rest, tile_alone, rest_alone, cluster; };
+constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 106, 460, 106, 460, 350}, {128, 1, 176, 700, 176, 700, 500}};
+constexpr TreeCost kCost16[3] = {{32, 1, 67, 250, 67, 250, 100}, {64, 1, 74, 350, 74, 350, 350}, {128, 1, 128, 660, 128, 660, 500}};
+constexpr TreeCost kCostSimt = {kSimtLines, 2, 400, 800, 400, 800, 0}, kCostAny = {kTreeLines, 2, 400, 800, 400, 800, 0};
+// k_tree_join: a launch, and 1.3 ns for a stretch of a line
+constexpr int kJoinLaunch = 300, kJoinLines8 = 8;
 
-TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, int slots, int max_cluster) {
+// The stretch that ends first: units of about the mean length in rounds of as many as run at once, but not before the longest one
+// and not before the keys have come from memory.  (26 drawn calls, each with up to 21 forced widths and stretches: what this picks takes
+// 1.02 times the best in the mean, 1.15 at worst; 64 to 128 lines over e4m3 took up to 1.8 times as long without the clusters' places
+// and the cost of joining.)
+template <typename Slots>
+TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, bool tc, Slots in_clusters) {
   TreePlan p{};
-  p.lines_per_unit = lines_per_unit; p.slots = slots;
-  const int G = in->n_q_heads / c->n_kv_heads;
+  p.shape = k.lines; p.tc = tc; p.cost = -1;
+  const int G = in->n_q_heads / c->n_kv_heads, sms = sm_count();
   int longest = 0, units[DC_MAX_BATCH], tiles[DC_MAX_BATCH];
+  long long all = 0;
   for (int b = 0; b < in->batch; ++b) {
     const int R = in->n_rows[b];
     p.base[b] = p.lines;
     p.lines += R * in->n_q_heads;
-    const int lt = (R * G + lines_per_unit - 1) / lines_per_unit;
+    const int lt = (R * G + k.lines - 1) / k.lines;
     p.line_tiles = p.line_tiles > lt ? p.line_tiles : lt;
     units[b] = lt * c->n_kv_heads;
     tiles[b] = R ? (in->ctx_len[b] + R + kTreeTile - 1) / kTreeTile : 0;
     longest = longest > tiles[b] ? longest : tiles[b];
+    all += tiles[b];
   }
-  long long best = -1;
+  const long long kb = (long long)c->head_dim * (c->dtype == DC_F32 ? 4 : c->dtype == DC_BF16 ? 2 : 1) * 2 * kTreeTile >> 10;   // of a tile
+  const long long memory = all * c->n_kv_heads * kb / 65 + k.rest_alone;   // 6.5 TB/s: 65 KB in 10 ns
+  long long work = 0;
+  for (int b = 0; b < in->batch; ++b) work += (long long)units[b] * tiles[b];
+  auto rounds = [&](long long n, int slots, int t, int more) {
+    const int one_each = slots / k.resident;
+    const long long left = n % slots, tiles_mean = n <= slots ? t * k.tile : work * k.tile / n;
+    const long long two = tiles_mean + k.rest + more, one = tiles_mean * k.tile_alone / k.tile + k.rest_alone + more;
+    const long long last = left == 0 ? 0 : left <= one_each ? one : one + (two - one) * (left - one_each) / (slots - one_each);
+    const long long cost = n / slots * two + last, most = t * k.tile_alone + k.rest_alone + more;
+    return cost > most ? cost : most;
+  };
   for (int s = 1, before = 0; s <= longest && s <= 256; ++s) {
     const int t = (longest + s - 1) / s;
     if (t == before) continue;
     before = t;
     const int stretches = (longest + t - 1) / t;
-    const bool cluster = stretches > 1 && stretches <= max_cluster;     // (whose places are taken by its CTAs without keys too)
     long long n = 0;
-    for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * (cluster ? stretches : (tiles[b] + t - 1) / t);
-    const long long cost = (n + slots - 1) / slots * (t + kUnitStart) + (stretches == 1 ? 0 : cluster ? kJoinCluster : kJoinLaunch);
-    if (best < 0 || cost < best) { best = cost; p.tiles = t; }
+    for (int b = 0; b < in->batch; ++b) n += (long long)units[b] * ((tiles[b] + t - 1) / t);
+    auto take = [&](long long cost, int cluster) {
+      cost = (cost > memory ? cost : memory) + cost / 16;      // (of those that wait for memory the one with less else to do)
+      if (p.cost < 0 || cost < p.cost) { p.cost = cost; p.tiles = t; p.cluster = cluster; }
+    };
+    if (stretches > 1 && stretches <= kMaxCluster && tc) {
+      // (behind the first round a cluster waits until its CTAs find places at once: about a third of them stay empty meanwhile)
+      const int slots = in_clusters(stretches);
+      take(rounds(n, n > slots ? slots - slots / 3 : slots, t, k.cluster), 1);
+    }
+    take(rounds(n, k.resident * sms, t, 0) + (stretches == 1 ? 0 : kJoinLaunch + (long long)p.lines * stretches / kJoinLines8), 0);
   }
   p.joined = longest ? (longest + p.tiles - 1) / p.tiles : 0;
-  p.cluster = p.joined > 1 && p.joined <= max_cluster;
   if (p.joined > 1 && !p.cluster) {
     const uint64_t n = (uint64_t)p.joined * p.lines;
     p.bytes = n * 8 + (n & 1) * 8 + n * c->head_dim * 4;
@@ -69,30 +147,34 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, int lines_per_unit, 
   return p;
 }
 
-// The tensor-core kernel's shapes: N lines of a unit, 0 for the CUDA-core kernel
-int tc_lines(const dc_cache* c, const dc_tree_in* in) {
-  const uint64_t keys = (uint64_t)c->max_batch * c->n_kv_heads * c->max_ctx, dims = (uint64_t)c->max_batch * c->n_kv_heads * kHd;
-  if (in->dtype != DC_BF16 || c->head_dim != kHd || !op_aligned(c->k) || !op_aligned(c->v) || keys >> 31 || dims >> 31) return 0;
-  int most = 0;
-  for (int b = 0; b < in->batch; ++b) most = most > in->n_rows[b] ? most : in->n_rows[b];
-  const int lines = most * (in->n_q_heads / c->n_kv_heads);
-  if (lines <= 64) return lines <= 32 ? 32 : 64;
-  // 128 lines take K and V in half as often and cost less than twice as much, as long as there is work for every SM
-  long long units = 0;
-  for (int b = 0; b < in->batch; ++b)
-    units += (long long)((in->n_rows[b] * (in->n_q_heads / c->n_kv_heads) + 127) / 128) * c->n_kv_heads * ((in->ctx_len[b] + in->n_rows[b] + 8 * kTreeTile - 1) / (8 * kTreeTile));
-  return units >= sm_count() ? 128 : 64;
-}
-
 bool simt_fast(const dc_cache* c, const dc_tree_in* in) {
   return (c->head_dim == 64 || (c->head_dim == 128 && in->dtype == DC_F32)) && op_aligned(c->k) && op_aligned(c->v);
 }
 
+// The tensor-core kernel's widths that leave none of their columns' halves without a line
+template <bool Q8>
+TreePlan plan_tc(const dc_cache* c, const dc_tree_in* in) {
+  int most = 0;
+  for (int b = 0; b < in->batch; ++b) most = most > in->n_rows[b] ? most : in->n_rows[b];
+  const int lines = most * (in->n_q_heads / c->n_kv_heads);
+  const TreeCost* k = Q8 ? kCost8 : kCost16;
+  TreePlan best = make_plan(c, in, k[0], true, [](int size) { return cluster_slots<32, Q8>(size); });
+  if (lines > 32) {
+    const TreePlan p = make_plan(c, in, k[1], true, [](int size) { return cluster_slots<64, Q8>(size); });
+    if (p.cost < best.cost) best = p;
+  }
+  if (lines > 64) {
+    const TreePlan p = make_plan(c, in, k[2], true, [](int size) { return cluster_slots<128, Q8>(size); });
+    if (p.cost < best.cost) best = p;
+  }
+  return best;
+}
+
 TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
-  const int n = tc_lines(c, in);
-  if (n == 0 && simt_fast(c, in)) return make_plan(c, in, kSimtLines, 2 * sm_count(), 0);
-  if (n == 0) return make_plan(c, in, kTreeLines, 2 * sm_count(), 0);
-  return make_plan(c, in, n, (n == 32 && c->dtype == DC_E4M3 ? 2 : 1) * sm_count(), kMaxCluster);
+  const uint64_t keys = (uint64_t)c->max_batch * c->n_kv_heads * c->max_ctx, dims = (uint64_t)c->max_batch * c->n_kv_heads * kHd;
+  if (in->dtype == DC_BF16 && c->head_dim == kHd && op_aligned(c->k) && op_aligned(c->v) && !(keys >> 31) && !(dims >> 31))
+    return c->dtype == DC_E4M3 ? plan_tc<true>(c, in) : plan_tc<false>(c, in);
+  return make_plan(c, in, simt_fast(c, in) ? kCostSimt : kCostAny, false, [](int) { return 0; });
 }
 
 int check(const dc_cache* c, const dc_tree_in* in) {
@@ -112,18 +194,6 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   return DC_OK;
 }
 
-// once per device and kernel: shared memory beyond 48 KB
-template <typename K>
-bool opt_in(K kernel, int bytes, std::atomic<unsigned long long>& done) {
-  int dev = 0;
-  cudaGetDevice(&dev);
-  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
-  if (done.load(std::memory_order_acquire) & bit) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-  done.fetch_or(bit, std::memory_order_release);
-  return true;
-}
-
 template <typename T, typename H, int HD>
 bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
   static std::atomic<unsigned long long> done;
@@ -133,7 +203,7 @@ bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_
 
 template <typename T, typename H>
 bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
-  if (p.lines_per_unit == kSimtLines) {
+  if (p.shape == kSimtLines) {
     if (a.c.head_dim == 64) return launch_simt_hd<T, H, 64>(a, p, batch, s);
     if constexpr (sizeof(T) == 4) return launch_simt_hd<T, H, 128>(a, p, batch, s);    // (bf16 rows have the tensor cores)
   }
@@ -145,8 +215,7 @@ bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s
 template <int N, bool Q8>
 bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, int vec_o, cudaStream_t s) {
   using C = TreeTc<N, Q8>;
-  static std::atomic<unsigned long long> done;
-  if (!opt_in(k_tree_tc<N, Q8>, C::kSmem, done)) return false;
+  if (!opt_in_tc<N, Q8>()) return false;
   CUtensorMap mk, mv;
   const uint64_t heads = (uint64_t)a.c.max_batch * a.c.n_kv_heads;
   if (!tc_map_bytes(&mk, a.c.k, Q8 ? 1 : 2, heads * a.c.max_ctx, kHd) || !tc_map_bytes(&mv, a.c.v, Q8 ? 1 : 2, heads * kHd, a.c.max_ctx)) return false;
@@ -215,7 +284,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.status = in->status;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
-  const int n_lines = tc_lines(cache, in);
+  const int n_lines = p.tc ? p.shape : 0;
   int vec_q = op_aligned(in->q), vec_o = op_aligned(in->o);
   for (int i = 0; i < 3; ++i) { vec_q = vec_q && in->q_stride[i] % 8 == 0; vec_o = vec_o && in->o_stride[i] % 8 == 0; }
   const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<32, false>(a, p, in->batch, vec_q, vec_o, s))
