@@ -78,11 +78,6 @@ __global__ void __launch_bounds__(kQkThreads) k_qk_any(const __grid_constant__ Q
 template <typename T> constexpr int kQkVecThreads = sizeof(T) == 4 ? 256 : 512;      // two or three of these CTAs to an SM
 template <typename T> constexpr int kQkVecCtas = sizeof(T) == 4 ? 3 : 2;
 
-__device__ __forceinline__ ptx::f32x2 qk_mul2(ptx::f32x2 a, ptx::f32x2 b) {
-  ptx::f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 constexpr int kQkDepth = 4;
 __device__ __forceinline__ void qk_copy16(uint4* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
@@ -224,8 +219,8 @@ __global__ void __launch_bounds__(kQkVecThreads<T>, kQkVecCtas<T>) k_qk_vec(cons
         const ulonglong2 A = two(0), B = two(1), Cc = two(2), D = two(3);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const ptx::f32x2 ur = qk_mul2(u2[i + e], r2), vr = qk_mul2(v2[i + e], r2);
-          const ptx::f32x2 p = ptx::f2_fma(ur, e ? A.y : A.x, qk_mul2(vr, e ? B.y : B.x)), q = ptx::f2_fma(vr, e ? Cc.y : Cc.x, qk_mul2(ur, e ? D.y : D.x));
+          const ptx::f32x2 ur = ptx::f2_mul(u2[i + e], r2), vr = ptx::f2_mul(v2[i + e], r2);
+          const ptx::f32x2 p = ptx::f2_fma(ur, e ? A.y : A.x, ptx::f2_mul(vr, e ? B.y : B.x)), q = ptx::f2_fma(vr, e ? Cc.y : Cc.x, ptx::f2_mul(ur, e ? D.y : D.x));
           ptx::f2_unpack(p, y0[2 * (i + e)], y0[2 * (i + e) + 1]);
           ptx::f2_unpack(q, y1[2 * (i + e)], y1[2 * (i + e) + 1]);
         }

@@ -169,11 +169,6 @@ __device__ __forceinline__ void tree_split4(__half2 x, __half2 y, uint32_t& hi, 
 __device__ __forceinline__ __half2 tree_half2(uint32_t e4m3x2) {
   return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)e4m3x2, __NV_E4M3));
 }
-__device__ __forceinline__ ptx::f32x2 tree_mul2(ptx::f32x2 a, ptx::f32x2 b) {
-  ptx::f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 
 // A bounded wait as ptx::mbar_wait, without the hint that lets a try sleep: the warps here wait little, and a try with the
 // hint is a loop of its own, whose instructions the softmax warps of the other CTA on the SM would have to share with.
@@ -575,7 +570,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         ptx::f32x2 s0 = ptx::f2_pack(v[i], v[i + 1]), s1 = ptx::f2_pack(v[i + 2], v[i + 3]);
         if (Q8) {
           const ulonglong2 rs = *reinterpret_cast<const ulonglong2*>(&c.rs[col + i]);
-          s0 = tree_mul2(s0, rs.x); s1 = tree_mul2(s1, rs.y);
+          s0 = ptx::f2_mul(s0, rs.x); s1 = ptx::f2_mul(s1, rs.y);
           s0 = ptx::f2_fma(s0, mul2, ptx::f2_add(off2, m2.x)); s1 = ptx::f2_fma(s1, mul2, ptx::f2_add(off2, m2.y));
         } else {
           s0 = ptx::f2_fma(s0, mul2, m2.x); s1 = ptx::f2_fma(s1, mul2, m2.y);
@@ -646,7 +641,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
         if (j > 0) {
 #pragma unroll
-          for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = tree_mul2(acc[i / 8][i % 8], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
+          for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = ptx::f2_mul(acc[i / 8][i % 8], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
           ptx::tc_fence_after();
 #pragma unroll 1
           for (int i = 0; i < (Q8 ? 2 * CW : CW); i += 4) {

@@ -69,8 +69,8 @@ int cluster_slots(int size) {
 
 // Units of one call: stretches of `tiles` tiles of keys, `line_tiles` stretches of lines a sequence.
 struct TreePlan {
+  enum Kind { kTc, kFast, kAny } kind;     // k_tree_tc, k_tree_simt_hd, k_tree_simt
   int shape;                 // lines of a unit
-  bool tc;
   int tiles, joined, line_tiles, cluster;
   int lines, base[DC_MAX_BATCH];
   uint64_t bytes;
@@ -83,7 +83,9 @@ struct TreePlan {
 struct TreeCost { int lines, resident, tile, rest, tile_alone, rest_alone, cluster; };
 constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 106, 460, 106, 460, 350}, {128, 1, 176, 700, 176, 700, 500}};
 constexpr TreeCost kCost16[3] = {{32, 1, 67, 250, 67, 250, 100}, {64, 1, 74, 350, 74, 350, 350}, {128, 1, 128, 660, 128, 660, 500}};
-constexpr TreeCost kCostSimt = {kSimtLines, 2, 400, 800, 400, 800, 0}, kCostAny = {kTreeLines, 2, 400, 800, 400, 800, 0};
+constexpr TreeCost kCost64[3] = {{8, 3, 860, 60, 757, 30, 0}, {32, 2, 996, 460, 962, 430, 0}, {64, 2, 1747, 1030, 1686, 980, 0}};    // k_tree_simt_hd
+constexpr TreeCost kCost128[3] = {{8, 3, 1650, 170, 1430, 180, 0}, {32, 2, 1889, 580, 1808, 600, 0}, {64, 1, 2714, 1080, 2714, 1080, 0}};
+constexpr TreeCost kCostAny = {kTreeLines, 2, 400, 800, 400, 800, 0};
 // k_tree_join: a launch, and 1.3 ns for a stretch of a line
 constexpr int kJoinLaunch = 300, kJoinLines8 = 8;
 
@@ -92,9 +94,9 @@ constexpr int kJoinLaunch = 300, kJoinLines8 = 8;
 // 1.02 times the best in the mean, 1.15 at worst; 64 to 128 lines over e4m3 took up to 1.8 times as long without the clusters' places
 // and the cost of joining.)
 template <typename Slots>
-TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, bool tc, Slots in_clusters) {
+TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, TreePlan::Kind kind, Slots in_clusters) {
   TreePlan p{};
-  p.shape = k.lines; p.tc = tc; p.cost = -1;
+  p.shape = k.lines; p.kind = kind; p.cost = -1;
   const int G = in->n_q_heads / c->n_kv_heads, sms = sm_count();
   int longest = 0, units[DC_MAX_BATCH], tiles[DC_MAX_BATCH];
   long long all = 0;
@@ -132,7 +134,7 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, b
       cost = (cost > memory ? cost : memory) + cost / 16;      // (of those that wait for memory the one with less else to do)
       if (p.cost < 0 || cost < p.cost) { p.cost = cost; p.tiles = t; p.cluster = cluster; }
     };
-    if (stretches > 1 && stretches <= kMaxCluster && tc) {
+    if (stretches > 1 && stretches <= kMaxCluster && kind == TreePlan::kTc) {
       // (behind the first round a cluster waits until its CTAs find places at once: about a third of them stay empty meanwhile)
       const int slots = in_clusters(stretches);
       take(rounds(n, n > slots ? slots - slots / 3 : slots, t, k.cluster), 1);
@@ -151,30 +153,36 @@ bool simt_fast(const dc_cache* c, const dc_tree_in* in) {
   return (c->head_dim == 64 || (c->head_dim == 128 && in->dtype == DC_F32)) && op_aligned(c->k) && op_aligned(c->v);
 }
 
-// The tensor-core kernel's widths that leave none of their columns' halves without a line
-template <bool Q8>
-TreePlan plan_tc(const dc_cache* c, const dc_tree_in* in) {
+// Widths in rising order, the next one where the one before has not room for all lines
+template <typename Slots0, typename Slots1, typename Slots2>
+TreePlan plan_widths(const dc_cache* c, const dc_tree_in* in, const TreeCost (&k)[3], TreePlan::Kind kind, Slots0 s0, Slots1 s1, Slots2 s2) {
   int most = 0;
   for (int b = 0; b < in->batch; ++b) most = most > in->n_rows[b] ? most : in->n_rows[b];
   const int lines = most * (in->n_q_heads / c->n_kv_heads);
-  const TreeCost* k = Q8 ? kCost8 : kCost16;
-  TreePlan best = make_plan(c, in, k[0], true, [](int size) { return cluster_slots<32, Q8>(size); });
-  if (lines > 32) {
-    const TreePlan p = make_plan(c, in, k[1], true, [](int size) { return cluster_slots<64, Q8>(size); });
+  TreePlan best = make_plan(c, in, k[0], kind, s0);
+  if (lines > k[0].lines) {
+    const TreePlan p = make_plan(c, in, k[1], kind, s1);
     if (p.cost < best.cost) best = p;
   }
-  if (lines > 64) {
-    const TreePlan p = make_plan(c, in, k[2], true, [](int size) { return cluster_slots<128, Q8>(size); });
+  if (lines > k[1].lines) {
+    const TreePlan p = make_plan(c, in, k[2], kind, s2);
     if (p.cost < best.cost) best = p;
   }
   return best;
+}
+
+template <bool Q8>
+TreePlan plan_tc(const dc_cache* c, const dc_tree_in* in) {
+  return plan_widths(c, in, Q8 ? kCost8 : kCost16, TreePlan::kTc, cluster_slots<32, Q8>, cluster_slots<64, Q8>, cluster_slots<128, Q8>);
 }
 
 TreePlan plan(const dc_cache* c, const dc_tree_in* in) {
   const uint64_t keys = (uint64_t)c->max_batch * c->n_kv_heads * c->max_ctx, dims = (uint64_t)c->max_batch * c->n_kv_heads * kHd;
   if (in->dtype == DC_BF16 && c->head_dim == kHd && op_aligned(c->k) && op_aligned(c->v) && !(keys >> 31) && !(dims >> 31))
     return c->dtype == DC_E4M3 ? plan_tc<true>(c, in) : plan_tc<false>(c, in);
-  return make_plan(c, in, simt_fast(c, in) ? kCostSimt : kCostAny, false, [](int) { return 0; });
+  auto none = [](int) { return 0; };
+  if (simt_fast(c, in)) return plan_widths(c, in, c->head_dim == 64 ? kCost64 : kCost128, TreePlan::kFast, none, none, none);
+  return make_plan(c, in, kCostAny, TreePlan::kAny, none);
 }
 
 int check(const dc_cache* c, const dc_tree_in* in) {
@@ -194,16 +202,20 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   return DC_OK;
 }
 
-template <typename T, typename H, int HD>
+template <typename T, typename H, int HD, int L>
 bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
   static std::atomic<unsigned long long> done;
-  if (!opt_in(k_tree_simt_hd<T, H, HD>, tree_simt_smem_hd(HD), done)) return false;
-  return launch_chained(k_tree_simt_hd<T, H, HD>, dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), dim3(256), tree_simt_smem_hd(HD), s, a) == cudaSuccess;
+  if (!opt_in(k_tree_simt_hd<T, H, HD, L>, tree_simt_smem_hd(HD, L), done)) return false;
+  return launch_chained(k_tree_simt_hd<T, H, HD, L>, dim3(p.joined, a.c.n_kv_heads, batch * p.line_tiles), dim3(kSimtThreads), tree_simt_smem_hd(HD, L), s, a) == cudaSuccess;
+}
+template <typename T, typename H, int HD>
+bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
+  return p.shape == 8 ? launch_simt_hd<T, H, HD, 1>(a, p, batch, s) : p.shape == 32 ? launch_simt_hd<T, H, HD, 4>(a, p, batch, s) : launch_simt_hd<T, H, HD, 8>(a, p, batch, s);
 }
 
 template <typename T, typename H>
 bool launch_simt(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
-  if (p.shape == kSimtLines) {
+  if (p.kind == TreePlan::kFast) {
     if (a.c.head_dim == 64) return launch_simt_hd<T, H, 64>(a, p, batch, s);
     if constexpr (sizeof(T) == 4) return launch_simt_hd<T, H, 128>(a, p, batch, s);    // (bf16 rows have the tensor cores)
   }
@@ -284,7 +296,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   a.status = in->status;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
-  const int n_lines = p.tc ? p.shape : 0;
+  const int n_lines = p.kind == TreePlan::kTc ? p.shape : 0;
   int vec_q = op_aligned(in->q), vec_o = op_aligned(in->o);
   for (int i = 0; i < 3; ++i) { vec_q = vec_q && in->q_stride[i] % 8 == 0; vec_o = vec_o && in->o_stride[i] % 8 == 0; }
   const bool ok = n_lines == 32 ? (q8 ? launch_tc<32, true>(a, p, in->batch, vec_q, vec_o, s) : launch_tc<32, false>(a, p, in->batch, vec_q, vec_o, s))

@@ -7,6 +7,7 @@
 #pragma once
 #include "ops.h"
 #include "pdl.cuh"
+#include "tc_ptx.cuh"
 
 namespace dc {
 
@@ -86,19 +87,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_tree_join(const __grid_cons
 }
 
 // ---- CUDA cores, head_dim 64 or 128, cache on 16-byte boundaries ------------------------------------------
-// grid (stretch, kv head, sequence * line tiles); 256 threads, 32 lines, 64 keys at a time.  In both products a thread has 2 lines x 4
-// keys or 2 lines x HD/16 dims in registers and takes 6 to 10 16-byte loads from shared memory for 32 to 64 multiply-adds.  The next
-// keys are on their way while these are worked on.  4 x 2064 keys of 4 heads, 64 rows of 4 heads a group, fp32: 138 us, of which 30 are
-// multiply-adds at the full rate (two CTAs of 8 warps wait for shared memory); three CTAs an SM 150 us (spills).
-constexpr int kSimtLines = 32, kSimtKeys = 64;
-__host__ __device__ constexpr int tree_simt_smem_hd(int hd) {
-  return (kSimtLines * (hd + 4) + kSimtKeys * (hd + 4) + hd * (kSimtKeys + 4) + kSimtLines * (kSimtKeys + 4)) * 4;
+// grid (stretch, kv head, sequence * line tiles); 128 threads, 8 L lines (L of a thread: 8, or fewer where there are no more), 64 keys at
+// a time.  In both products a thread has L lines x 4 keys or L lines x HD/16 dims in registers, two neighbours along the sum in one
+// f32x2: with eight lines 12 16-byte loads from shared memory (an SM has four bytes a clock and lane) for 64 instructions of two multiply-adds.  Head_dim 64: the next keys' K
+// and V are on their way (fp32: straight to shared memory) while these are worked on; 128, where two tiles have no room: the next K
+// while V is worked on, and V while K is.  Drafted keys behind the last one that a line of the unit sees are left out.
+constexpr int kSimtKeys = 64, kSimtThreads = 128;
+__host__ __device__ constexpr int tree_simt_smem_hd(int hd, int l) {
+  return (8 * l * (hd + 4) + (hd == 64 ? 2 : 1) * (kSimtKeys * (hd + 4) + hd * (kSimtKeys + 4)) + 8 * l * (kSimtKeys + 4)) * 4;
 }
+constexpr int tree_simt_ctas(int hd, int l) { return l == 1 ? 3 : l == 8 && hd == 128 ? 1 : 2; }     // of an SM, as shared memory has room
 // 16 bytes of a cache as fp32
 template <typename H> __device__ __forceinline__ void tree_wide(const uint4& w, float (&x)[16 / sizeof(H)]);
-template <> __device__ __forceinline__ void tree_wide<float>(const uint4& w, float (&x)[4]) {
-  x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
-}
 template <> __device__ __forceinline__ void tree_wide<__nv_bfloat16>(const uint4& w, float (&x)[8]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -113,172 +113,264 @@ template <> __device__ __forceinline__ void tree_wide<__nv_fp8_e4m3>(const uint4
     x[2 * i] = f.x; x[2 * i + 1] = f.y;
   }
 }
+__device__ __forceinline__ void tree_copy16(float* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void tree_copies_in() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-template <typename T, typename H, int HD>
-__global__ void __launch_bounds__(256, 2) k_tree_simt_hd(const __grid_constant__ TreeArgs a) {
+template <typename T, typename H, int HD, int L>
+__global__ void __launch_bounds__(kSimtThreads, tree_simt_ctas(HD, L)) k_tree_simt_hd(const __grid_constant__ TreeArgs a) {
+  constexpr bool F32 = sizeof(H) == 4;
+  constexpr int kLines = 8 * L, kTiles = HD == 64 ? 2 : 1;        // tiles of K and V in shared memory
   constexpr int E = 16 / sizeof(H);                              // values of a load
-  constexpr int NL = kSimtKeys * HD / E / 256;                   // loads a thread has of K, and of V
+  constexpr int NL = kSimtKeys * HD / E / kSimtThreads;          // loads a thread has of K, and of V
   constexpr int DPT = HD / 16, KP = HD + 4, VP = kSimtKeys + 4;  // dims a thread; row pitches in shared memory
   extern __shared__ float tree_smem[];
   __shared__ uint32_t poison[8];
+  __shared__ int last_seen[kSimtThreads / 32];
+  __shared__ uint32_t masks[kLines][8];      // of the unit's lines, bits of drafted keys
   const int b = blockIdx.z / a.line_tiles, R = a.rows[b], G = a.group, nkv = a.c.n_kv_heads;
-  const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kSimtLines, n = min(kSimtLines, R * G - line0);
-  const int ctx = a.ctx[b], keys = ctx + R, k0 = blockIdx.x * a.tiles * kTreeTile, k1 = min(keys, k0 + a.tiles * kTreeTile);
+  const int g = blockIdx.y, line0 = (blockIdx.z - b * a.line_tiles) * kLines, n = min(kLines, R * G - line0);
+  const int ctx = a.ctx[b], keys = ctx + R, k0 = blockIdx.x * a.tiles * kTreeTile;
+  int k1 = min(keys, k0 + a.tiles * kTreeTile);
   pdl_trigger();
   pdl_wait();
   if (n <= 0 || k0 >= keys) return;
-  float *qs = tree_smem, *ks = qs + kSimtLines * KP, *vs = ks + kSimtKeys * KP, *ps = vs + HD * VP;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;     // keys 4 tx .. + 3 (dims tx, tx + 16, ..) of lines 2 ty, 2 ty + 1
+  constexpr int kTileFloats = kSimtKeys * KP + HD * VP;
+  float *qs = tree_smem, *ps = qs + kLines * KP, *tiles = ps + kLines * VP;
+  auto k_at = [&](int t) { return tiles + (kTiles == 2 ? (t - k0) / kSimtKeys % 2 * kTileFloats : 0); };
+  auto v_at = [&](int t) { return k_at(t) + kSimtKeys * KP; };
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;     // keys (dims) tx, tx + 16, .. of lines L ty .. + L - 1
   const size_t slot = (size_t)b * nkv + g;
   const H* K = static_cast<const H*>(a.c.k) + slot * a.c.max_ctx * HD;
   const H* V = static_cast<const H*>(a.c.v) + slot * a.c.max_ctx * HD;
   const float* k_scale = a.c.k_scale + slot * a.c.max_ctx;
   const float* v_scale = a.c.v_scale + slot * a.c.max_ctx;
-  uint4 kw[NL], vw[NL];
-  auto fetch = [&](int t) {
+  // (whole pieces of both: the cache goes on to a multiple of 64 keys)
+  uint4 kw[F32 ? 1 : NL], vw[F32 ? 1 : NL];
+  auto ask_k = [&](int t) {
+    float* ks = k_at(t);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int j = tid + 256 * i, key = j / (HD / E), d = j / (kSimtKeys / E);
-      kw[i] = t + key < k1 ? *reinterpret_cast<const uint4*>(K + (size_t)(t + key) * HD + j % (HD / E) * E) : make_uint4(0, 0, 0, 0);
-      // (whole pieces: the cache goes on to a multiple of 64 keys)
-      vw[i] = *reinterpret_cast<const uint4*>(V + (size_t)d * a.c.max_ctx + t + j % (kSimtKeys / E) * E);
+      const int j = tid + kSimtThreads * i, key = j / (HD / E), d = j % (HD / E) * E;
+      if constexpr (F32) tree_copy16(ks + key * KP + d, K + (size_t)(t + key) * HD + d);
+      else kw[i] = *reinterpret_cast<const uint4*>(K + (size_t)(t + key) * HD + d);
     }
   };
-  fetch(k0);
-  if (tid < 8) poison[tid] = 0;
-  for (int i = tid; i < kSimtLines * HD; i += 256) {
-    const int line = i / HD, m = line0 + line, r = tree_row(a, m);
-    qs[line * KP + i % HD] = line < n ? op_f32(static_cast<const T*>(a.q)[b * a.qs[0] + r * a.qs[1] + (g * G + m - r * G) * a.qs[2] + i % HD]) : 0.f;
-  }
-  const uint32_t* mask[2];
-#pragma unroll
-  for (int l = 0; l < 2; ++l) {
-    const int m = line0 + 2 * ty + l;
-    mask[l] = a.mask && 2 * ty + l < n ? a.mask + ((size_t)b * a.max_rows + tree_row(a, m)) * a.words : nullptr;
-  }
-  float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, o[2][DPT];
-#pragma unroll
-  for (int l = 0; l < 2; ++l)
-#pragma unroll
-    for (int i = 0; i < DPT; ++i) o[l][i] = 0.f;
-  for (int t = k0; t < k1; t += kSimtKeys) {
-    __syncthreads();
-    const bool drafted = a.mask && t + kSimtKeys > ctx;
+  auto ask_v = [&](int t) {
+    float* vs = v_at(t);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int j = tid + 256 * i, key = j / (HD / E), d = j / (kSimtKeys / E), first = j % (kSimtKeys / E) * E;
-      float x[E];
-      tree_wide<H>(kw[i], x);
-      const float sc = sizeof(H) == 1 && t + key < k1 ? k_scale[t + key] : 0.f;
+      const int j = tid + kSimtThreads * i, d = j / (kSimtKeys / E), key = j % (kSimtKeys / E) * E;
+      if constexpr (F32) tree_copy16(vs + d * VP + key, V + (size_t)d * a.c.max_ctx + t + key);
+      else vw[i] = *reinterpret_cast<const uint4*>(V + (size_t)d * a.c.max_ctx + t + key);
+    }
+  };
+  auto put_k = [&](int t) {
+    if constexpr (!F32) {
+      float* ks = k_at(t);
 #pragma unroll
-      for (int e = 0; e < E; e += 4) {
-        float4 w = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-        if (sizeof(H) == 1) { w.x *= sc; w.y *= sc; w.z *= sc; w.w *= sc; }
-        *reinterpret_cast<float4*>(ks + key * KP + j % (HD / E) * E + e) = w;
+      for (int i = 0; i < NL; ++i) {
+        const int j = tid + kSimtThreads * i, key = j / (HD / E), d = j % (HD / E) * E;
+        float x[E];
+        tree_wide<H>(kw[i], x);
+        const float sc = sizeof(H) == 1 ? k_scale[t + key] : 1.f;
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(ks + key * KP + d + e) = make_float4(x[e] * sc, x[e + 1] * sc, x[e + 2] * sc, x[e + 3] * sc);
       }
-      tree_wide<H>(vw[i], x);
+    }
+  };
+  auto put_v = [&](int t) {
+    if constexpr (!F32) {
+      float* vs = v_at(t);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int at = t + first + e;
-        if (at >= k1) x[e] = 0.f;            // whatever the cache holds there
-        else if (sizeof(H) == 1) x[e] *= v_scale[at];
-        // a drafted key's value that is not finite: 0 times it would be NaN for lines that do not see the key
-        if (drafted && at >= ctx && at < k1 && !(fabsf(x[e]) <= 3.402823466e38f)) {
-          x[e] = 0.f;
+      for (int i = 0; i < NL; ++i) {
+        const int j = tid + kSimtThreads * i, d = j / (kSimtKeys / E), key = j % (kSimtKeys / E) * E;
+        float x[E];
+        tree_wide<H>(vw[i], x);
+        if constexpr (sizeof(H) == 1) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] *= v_scale[t + key + e];
+        }
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(vs + d * VP + key + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      }
+    }
+  };
+  ask_k(k0);
+  if (!F32 || kTiles == 2) ask_v(k0);
+  if (tid < 8) poison[tid] = 0;
+  constexpr int kAsk = kLines * HD / kSimtThreads < 16 ? kLines * HD / kSimtThreads : 16;      // queries of a thread that are on their way at once
+#pragma unroll 1
+  for (int i0 = tid; i0 < kLines * HD; i0 += kAsk * kSimtThreads) {
+    float x[kAsk];
+#pragma unroll
+    for (int i = 0; i < kAsk; ++i) {
+      const int line = (i0 + i * kSimtThreads) / HD, d = i0 % HD, m = line0 + line, r = tree_row(a, m);
+      x[i] = line < n ? op_f32(static_cast<const T*>(a.q)[b * a.qs[0] + r * a.qs[1] + (g * G + m - r * G) * a.qs[2] + d]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kAsk; ++i) qs[(i0 + i * kSimtThreads) / HD * KP + i0 % HD] = x[i];
+  }
+  if (a.mask) {
+    int last = -1;
+    for (int i = tid; i < kLines * 8; i += kSimtThreads) {
+      const int line = i >> 3, w = i & 7, left = R - 32 * w;
+      uint32_t bits = 0u;
+      if (line < n && left > 0) {
+        bits = a.mask[((size_t)b * a.max_rows + tree_row(a, line0 + line)) * a.words + w];
+        if (left < 32) bits &= (1u << left) - 1u;
+      }
+      masks[line][w] = bits;
+      if (bits) last = max(last, 32 * w + 31 - __clz(bits));
+    }
+    last = __reduce_max_sync(0xffffffffu, last);
+    if (tid % 32 == 0) last_seen[tid / 32] = last;
+    __syncthreads();
+    k1 = min(k1, ctx + max(max(last_seen[0], last_seen[1]), max(last_seen[2], last_seen[3])) + 1);
+  }
+  float top[L], sum[L];
+  ptx::f32x2 o[L][DPT];
+#pragma unroll
+  for (int l = 0; l < L; ++l) {
+    top[l] = -INFINITY; sum[l] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DPT; ++i) o[l][i] = 0ull;
+  }
+  auto in_order = [&](int t) {
+    if (t + kSimtKeys > k1 || (a.mask && t + kSimtKeys > ctx)) {
+      // whatever the cache holds behind the last key, and a drafted key's values that are not finite: 0 times them would be NaN for
+      // lines that do not see the key
+      for (int i = tid; i < HD * kSimtKeys; i += kSimtThreads) {
+        float& x = v_at(t)[i / kSimtKeys * VP + i % kSimtKeys];
+        const int at = t + i % kSimtKeys;
+        if (at >= k1) x = 0.f;
+        else if (a.mask && at >= ctx && !(fabsf(x) <= 3.402823466e38f)) {
+          x = 0.f;
           atomicOr(&poison[(at - ctx) >> 5], 1u << ((at - ctx) & 31));
         }
       }
-#pragma unroll
-      for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(vs + d * VP + first + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      __syncthreads();
     }
-    __syncthreads();
-    if (t + kSimtKeys < k1) fetch(t + kSimtKeys);
-    if (tid / 32 * 4 >= n) continue;      // (a warp without lines: the others have the pipes for themselves)
-    // scores
-    float z[2][4];
+  };
+  const bool idle = tid / 32 * 2 * L >= n;      // (a warp without lines: the others have the pipes for themselves)
+  for (int t = k0; t < k1; t += kSimtKeys) {
+    const bool more = t + kSimtKeys < k1;
+    const float *ks = k_at(t), *vs = v_at(t);
+    put_k(t);
+    if (kTiles == 2) put_v(t);
+    tree_copies_in();
+    __syncthreads();           // K (both) is there, and the keys before have been read
+    if (kTiles == 2) {
+      if (more) { ask_k(t + kSimtKeys); ask_v(t + kSimtKeys); }
+      in_order(t);
+    } else if (F32) {
+      ask_v(t);
+    } else {
+      put_v(t);
+      if (more) { ask_k(t + kSimtKeys); ask_v(t + kSimtKeys); }
+    }
+    if (!idle) {
+      ptx::f32x2 z2[L][4];
 #pragma unroll
-    for (int l = 0; l < 2; ++l)
+      for (int l = 0; l < L; ++l)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) z[l][e] = 0.f;
+        for (int e = 0; e < 4; ++e) z2[l][e] = 0ull;
 #pragma unroll 4
-    for (int d = 0; d < HD; d += 4) {
-      float4 q[2], x[4];
+      for (int d = 0; d < HD; d += 4) {
+        ulonglong2 q[L], x[4];
 #pragma unroll
-      for (int l = 0; l < 2; ++l) q[l] = *reinterpret_cast<const float4*>(qs + (2 * ty + l) * KP + d);
-      // (keys tx, tx + 16, ..: neighbours in shared memory rows go to different banks)
+        for (int l = 0; l < L; ++l) q[l] = *reinterpret_cast<const ulonglong2*>(qs + (L * ty + l) * KP + d);
+        // (keys tx, tx + 16, ..: neighbours in shared memory rows go to different banks)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(ks + (tx + 16 * e) * KP + d);
+        for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * e) * KP + d);
 #pragma unroll
-      for (int l = 0; l < 2; ++l)
+        for (int l = 0; l < L; ++l)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          z[l][e] = fmaf(q[l].x, x[e].x, fmaf(q[l].y, x[e].y, fmaf(q[l].z, x[e].z, fmaf(q[l].w, x[e].w, z[l][e]))));
-    }
-    // probabilities: the 16 threads of a line pair have its keys
-#pragma unroll
-    for (int l = 0; l < 2; ++l) {
-      float now = top[l];
-      bool any = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = t + tx + 16 * e, j = key - ctx;
-        bool sees = key < k1;
-        if (sees && j >= 0 && mask[l]) sees = (mask[l][j >> 5] >> (j & 31)) & 1u;
-        any = any || sees;
-        z[l][e] = sees ? z[l][e] * a.scale_log2 : -INFINITY;
-        now = fmaxf(now, z[l][e]);
-        ps[(2 * ty + l) * VP + tx + 16 * e] = sees ? 1.f : 0.f;
+          for (int e = 0; e < 4; ++e) z2[l][e] = ptx::f2_fma(q[l].y, x[e].y, ptx::f2_fma(q[l].x, x[e].x, z2[l][e]));
       }
+      // probabilities: the 16 threads of some lines have their keys
+      const bool all = t + kSimtKeys <= min(ctx, k1) || (!a.mask && t + kSimtKeys <= k1);
 #pragma unroll
-      for (int s = 8; s >= 1; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
-      const float f = top[l] == -INFINITY ? 0.f : exp2f(top[l] - now);
-      sum[l] *= f;
+      for (int l = 0; l < L; ++l) {
+        float z[4], now = top[l];
+        uint32_t sees = 0xfu;
+        if (!all) {
+          sees = 0u;
 #pragma unroll
-      for (int i = 0; i < DPT; ++i) o[l][i] *= f;
-      top[l] = now;
+          for (int e = 0; e < 4; ++e) {
+            const int key = t + tx + 16 * e, j = key - ctx;
+            if (key < k1 && (j < 0 || !a.mask || (masks[L * ty + l][j >> 5] >> (j & 31) & 1u))) sees |= 1u << e;
+          }
+        }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float& place = ps[(2 * ty + l) * VP + tx + 16 * e];
-        const float p = place != 0.f ? exp2f(z[l][e] - now) : 0.f;    // (a NaN score stays one)
-        sum[l] += p;
-        place = p;
+        for (int e = 0; e < 4; ++e) {
+          float odd;
+          ptx::f2_unpack(z2[l][e], z[e], odd);
+          z[e] = sees >> e & 1u ? (z[e] + odd) * a.scale_log2 : -INFINITY;
+          now = fmaxf(now, z[e]);
+        }
+#pragma unroll
+        for (int s = 8; s >= 1; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
+        const float f = top[l] == -INFINITY ? 0.f : exp2f(top[l] - now);
+        sum[l] *= f;
+        const ptx::f32x2 f2 = ptx::f2_pack(f, f);
+#pragma unroll
+        for (int i = 0; i < DPT; ++i) o[l][i] = ptx::f2_mul(o[l][i], f2);
+        top[l] = now;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = sees >> e & 1u ? exp2f(z[e] - now) : 0.f;    // (a NaN score stays one)
+          sum[l] += p;
+          ps[(L * ty + l) * VP + tx + 16 * e] = p;
+        }
       }
     }
-    __syncwarp();    // (a line's probabilities are made and read by the same half warp)
+    if (kTiles == 1) {
+      tree_copies_in();
+      __syncthreads();         // V is there, and K has been read
+      if (F32 && more) ask_k(t + kSimtKeys);
+      in_order(t);
+    }
+    if (idle) continue;
+    __syncwarp();              // (a line's probabilities are made and read by the same half warp)
 #pragma unroll 2
     for (int k = 0; k < kSimtKeys; k += 4) {
-      float4 p[2];
+      ulonglong2 p[L];
 #pragma unroll
-      for (int l = 0; l < 2; ++l) p[l] = *reinterpret_cast<const float4*>(ps + (2 * ty + l) * VP + k);
+      for (int l = 0; l < L; ++l) p[l] = *reinterpret_cast<const ulonglong2*>(ps + (L * ty + l) * VP + k);
 #pragma unroll
       for (int i = 0; i < DPT; ++i) {
-        const float4 x = *reinterpret_cast<const float4*>(vs + (tx + 16 * i) * VP + k);
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(vs + (tx + 16 * i) * VP + k);
 #pragma unroll
-        for (int l = 0; l < 2; ++l) o[l][i] = fmaf(p[l].x, x.x, fmaf(p[l].y, x.y, fmaf(p[l].z, x.z, fmaf(p[l].w, x.w, o[l][i]))));
+        for (int l = 0; l < L; ++l) o[l][i] = ptx::f2_fma(p[l].y, x.y, ptx::f2_fma(p[l].x, x.x, o[l][i]));
       }
     }
+    __syncwarp();
   }
+  tree_copies_in();   // (of a unit that turned out to have no keys)
   __syncthreads();    // (what the last keys noted)
   const bool alone = tree_stretches(a, b) == 1;
 #pragma unroll
-  for (int l = 0; l < 2; ++l) {
+  for (int l = 0; l < L; ++l) {
     float s = sum[l];
 #pragma unroll
     for (int i = 8; i >= 1; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
-    if (2 * ty + l >= n) continue;
-    if (mask[l])
+    if (L * ty + l >= n) continue;
+    if (a.mask)
       for (int w = 0; w < a.words; ++w)
-        if (mask[l][w] & poison[w]) s = __uint_as_float(0x7fffffffu);
-    const int m = line0 + 2 * ty + l, r = tree_row(a, m), h = g * G + m - r * G;
-    if (alone) {
-      T* dst = static_cast<T*>(a.o) + b * a.os[0] + r * a.os[1] + h * a.os[2];
+        if (masks[L * ty + l][w] & poison[w]) s = __uint_as_float(0x7fffffffu);
+    const int m = line0 + L * ty + l, r = tree_row(a, m), h = g * G + m - r * G;
+    const size_t at = (size_t)blockIdx.x * a.lines + tree_line(a, b, r, h);
+    T* dst = static_cast<T*>(a.o) + b * a.os[0] + r * a.os[1] + h * a.os[2];
+    if (!alone && tx == 0) a.part_ml[at] = make_float2(top[l], s);
 #pragma unroll
-      for (int i = 0; i < DPT; ++i) dst[tx + 16 * i] = op_to<T>(s == 0.f ? 0.f : o[l][i] / s);
-    } else {
-      const size_t at = (size_t)blockIdx.x * a.lines + tree_line(a, b, r, h);
-      if (tx == 0) a.part_ml[at] = make_float2(top[l], s);
-#pragma unroll
-      for (int i = 0; i < DPT; ++i) a.part_o[at * HD + tx + 16 * i] = o[l][i];
+    for (int i = 0; i < DPT; ++i) {
+      float x, odd;
+      ptx::f2_unpack(o[l][i], x, odd);
+      x += odd;
+      if (alone) dst[tx + 16 * i] = op_to<T>(s == 0.f ? 0.f : x / s);
+      else a.part_o[at * HD + tx + 16 * i] = x;
     }
   }
 }
