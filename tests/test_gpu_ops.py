@@ -1,5 +1,8 @@
 """The operators around a cache on the GPU against 64 bits."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -343,6 +346,26 @@ def test_tree_attention_scores_that_climb(held):
     _check_tree(c, 1, q, ctx, rows, bools, out)
 
 
+def _drawn(seed, longest, most):
+    rng = np.random.RandomState(seed)
+    B = int(rng.randint(1, 5))
+    rows = [int(rng.randint(1, most + 1)) for _ in range(B)]
+    ctx = [int(2 ** rng.uniform(0, math.log2(longest))) if rng.rand() < 0.85 else 0 for _ in range(B)]
+    hkv = int(rng.choice([1, 2, 4]))
+    return ctx, rows, max(rows) + int(rng.randint(0, 3)), hkv * int(rng.choice([1, 2, 4, 7])), hkv, bool(rng.rand() < 0.7)
+
+
+@pytest.mark.parametrize("seed", range(16))
+@pytest.mark.parametrize("dtype,held,hd", [(BF16, E4M3, 128), (BF16, BF16, 128), (F32, F32, 64), (F32, F32, 128), (BF16, BF16, 64), (F32, E4M3, 64)])
+def test_tree_attention_drawn_shapes(dtype, held, hd, seed):
+    """Whatever width, stretch and join the sizes lead to: one row to 256, one key to thousands, lengths far apart."""
+    big = hd == 128 and dtype == BF16
+    ctx, rows, most, hq, hkv, tree = _drawn(100 + seed, (8000 if seed % 4 == 0 else 1500) if big else 1200, (256, 40, 6, 1)[seed % 4])
+    c, q, mask, bools = _tree_case(dtype, held, ctx, rows, most, hq, hkv, hd, tree, seed=seed)
+    out = dc.tree_attention(q.to(DEV), c, ctx, rows, None if mask is None else mask.to(DEV), layer=1)
+    _check_tree(c, 1, q, ctx, rows, bools, out)
+
+
 @pytest.mark.parametrize("held,hd", [(E4M3, 128), (BF16, 128), (BF16, 64)])
 def test_tree_attention_rows_without_a_key_and_any_mask(held, hd):
     """Masks that are no tree: bits above the diagonal, rows that see nothing (zeros), bits beyond the rows (not looked at)."""
@@ -512,6 +535,30 @@ def test_outputs_made_for_a_call_on_another_stream_belong_to_that_stream():
         got, (a, b) = dc.tree_attention(qd, c, [200], [24], md, layer=1, stream=side), dc.qk_norm_rope(h, h, pos, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(a, turned[0]) and torch.equal(b, turned[1])
+
+
+FIRST = """
+import torch, paper_2604_15750_b200 as dc
+c = dc.KvCache.empty(1, 2, 4, 4096, 128, dtype=torch.float8_e4m3fn)
+x, q = (torch.randn(s, device="cuda").to(torch.bfloat16) for s in ((2, 300, 4, 128), (2, 24, 8, 128)))
+pos, mask = torch.arange(48, dtype=torch.int32, device="cuda"), dc.tree_mask([[-1] + list(range(23))] * 2).cuda()
+out, qo, ko = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((48, 4, 128), dtype=torch.bfloat16, device="cuda")
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    dc.cache_write(c, x, x, [0, 0])
+    dc.qk_norm_rope(q.view(48, 8, 128), ko, pos, q_out=qo.view(48, 8, 128), k_out=ko)
+    dc.tree_attention(qo, c, [3000, 100], [24, 24], mask, out=out)
+g.replay()
+got = out.clone()
+dc.tree_attention(qo, c, [3000, 100], [24, 24], mask, out=out)
+assert torch.equal(got, out) and out.abs().sum() > 0
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """What a kernel's first launch sets up (shared memory, places of clusters, modules) is no work on the stream."""
+    r = subprocess.run([sys.executable, "-c", FIRST], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 def test_a_workspace_of_the_callers_own():
