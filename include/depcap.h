@@ -543,7 +543,8 @@ typedef struct dc_tree_in {
 } dc_tree_in;
 DC_API int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, void* cuda_stream);
 
-/* The workspace that dc_tree_attention wants for these lengths (pointers to device memory are not looked at, but for their alignment). */
+/* The workspace that dc_tree_attention wants for these lengths on the current device (pointers to device memory are not looked
+ * at, but for their alignment). */
 DC_API int dc_tree_attention_workspace(const dc_cache* cache, const dc_tree_in* in, uint64_t* bytes);
 
 /* The mask of a tree, on the host: parent[r] < r is the row that row r continues, -1 none (it continues the context).

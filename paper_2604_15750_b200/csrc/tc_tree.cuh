@@ -22,14 +22,15 @@
 // P lies in shared memory as the threads have it, a row of N values for a key (the product takes it with the lines as the
 // contiguous axis): a thread stores 16 bytes at a time, where rows of keys would take a store for every value.
 //
-// Measured (device time): 16 x 4096 keys of 32 heads, 32 rows, e4m3, 566 MB: 99 us, 5.7 TB/s; 8 x 900..1200 keys, 24 rows, 77 MB: 20.8
-// us (3.7 TB/s; a unit's start and end are a third); 4 x 768 keys of 4 heads, 64 rows of 7 heads a group, bf16: 10.8 us (seven
-// tiles one after the other, 1250 clk each); one row over 512 keys of 32 heads: 8.1 us.
+// Measured (device time): 16 x 4096 keys of 32 heads, 32 rows, e4m3, 566 MB: 99 us, 5.7 TB/s; 8 x 900..1200 keys, 24 rows, 77 MB: 20.4
+// us (3.8 TB/s; a unit's start and end are a third); 4 x 768 keys of 4 heads, 64 rows of 7 heads a group, bf16: 10.9 us (seven
+// tiles one after the other, 1250 clk each); one row over 512 keys of 32 heads: 8.0 us.
 //
 // Why N = 32, 64 or 128: a column costs softmax time whether it has a line or not, and every further unit streams the keys again.
-// 32 lines and e4m3 leave room for two CTAs on an SM, whose starts and softmax overlap.  128 lines (where there is work for every
-// SM) take in 64 KB of bf16 a tile for twice as many: 4 x 4000 keys, 128 rows of 7 heads 67 -> 52 us; over e4m3 no gain (250 us for
-// 12 x 4635 keys, 121 rows of 4 heads): there the softmax bounds.
+// 32 lines and e4m3 leave room for two CTAs on an SM, whose starts and softmax overlap.  128 lines take in 64 KB of bf16 a tile for
+// four times as many as 32: 4 x 4000 keys, 128 rows of 7 heads 52 us, with 64 lines 67.  Over e4m3 a line costs about the same in all
+// three (0.89 us a tile of 64 lines with 128, 1.06 with 64, 1.1 with 32): there the softmax bounds (12 x 4635 keys of 8 heads, 121 rows
+// of 4 heads a group 221 us, 144 with half the heads).  Which one is taken: kCost8, kCost16 (tree_attn.cu).
 //
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them

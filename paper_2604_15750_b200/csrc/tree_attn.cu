@@ -62,6 +62,7 @@ int cluster_slots(int size) {
     }
     // (it counts one CTA an SM; where two have room, they do run: 256 CTAs of pairs took one round)
     v = v < 1 ? size : v * size * C::kResident;
+    v = v > sm_count() * C::kResident ? sm_count() * C::kResident : v;
     if (dev < 64) known[dev][size].store(v, std::memory_order_relaxed);
   }
   return v;
@@ -83,9 +84,9 @@ struct TreePlan {
 struct TreeCost { int lines, resident, tile, rest, tile_alone, rest_alone, cluster; };
 constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 106, 460, 106, 460, 350}, {128, 1, 176, 700, 176, 700, 500}};
 constexpr TreeCost kCost16[3] = {{32, 1, 67, 250, 67, 250, 100}, {64, 1, 74, 350, 74, 350, 350}, {128, 1, 128, 660, 128, 660, 500}};
-constexpr TreeCost kCost64[3] = {{8, 3, 860, 60, 757, 30, 0}, {32, 2, 996, 460, 962, 430, 0}, {64, 2, 1747, 1030, 1686, 980, 0}};    // k_tree_simt_hd
-constexpr TreeCost kCost128[3] = {{8, 3, 1650, 170, 1430, 180, 0}, {32, 2, 1889, 580, 1808, 600, 0}, {64, 1, 2714, 1080, 2714, 1080, 0}};
-constexpr TreeCost kCostAny = {kTreeLines, 2, 400, 800, 400, 800, 0};
+constexpr TreeCost kCost64[3] = {{8, 3, 870, 30, 760, 30, 0}, {32, 2, 980, 230, 950, 200, 0}, {64, 2, 1744, 610, 1680, 570, 0}};    // k_tree_simt_hd
+constexpr TreeCost kCost128[3] = {{8, 3, 1640, 50, 1430, 30, 0}, {32, 2, 1820, 420, 1750, 390, 0}, {64, 1, 2535, 770, 2535, 770, 0}};
+constexpr TreeCost kCostAny = {kTreeLines, 2, 2000, 500, 2000, 500, 0};
 // k_tree_join: a launch, and 1.3 ns for a stretch of a line
 constexpr int kJoinLaunch = 300, kJoinLines8 = 8;
 
@@ -117,8 +118,8 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, T
   for (int b = 0; b < in->batch; ++b) work += (long long)units[b] * tiles[b];
   auto rounds = [&](long long n, int slots, int t, int more) {
     const int one_each = slots / k.resident;
-    const long long left = n % slots, tiles_mean = n <= slots ? t * k.tile : work * k.tile / n;
-    const long long two = tiles_mean + k.rest + more, one = tiles_mean * k.tile_alone / k.tile + k.rest_alone + more;
+    const long long left = n % slots, mean = n <= slots ? t * k.tile : work * k.tile / n;
+    const long long two = mean + k.rest + more, one = mean * k.tile_alone / k.tile + k.rest_alone + more;
     const long long last = left == 0 ? 0 : left <= one_each ? one : one + (two - one) * (left - one_each) / (slots - one_each);
     const long long cost = n / slots * two + last, most = t * k.tile_alone + k.rest_alone + more;
     return cost > most ? cost : most;

@@ -92,6 +92,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_tree_join(const __grid_cons
 // f32x2: with eight lines 12 16-byte loads from shared memory (an SM has four bytes a clock and lane) for 64 instructions of two multiply-adds.  Head_dim 64: the next keys' K
 // and V are on their way (fp32: straight to shared memory) while these are worked on; 128, where two tiles have no room: the next K
 // while V is worked on, and V while K is.  Drafted keys behind the last one that a line of the unit sees are left out.
+// fp32, 64 rows of 4 heads a group, 4 x 2064 keys of 4 heads: head_dim 64 105 us, 128 183 us (2 lines x 4 keys a thread and single
+// multiply-adds 137 and 264): 45% of the multiply-adds' full rate, because two to three CTAs of four warps do not hide the latency of
+// shared memory, and more have no room.  9 rows, 14 x 2260 keys: 87 us (133).
 constexpr int kSimtKeys = 64, kSimtThreads = 128;
 __host__ __device__ constexpr int tree_simt_smem_hd(int hd, int l) {
   return (8 * l * (hd + 4) + (hd == 64 ? 2 : 1) * (kSimtKeys * (hd + 4) + hd * (kSimtKeys + 4)) + 8 * l * (kSimtKeys + 4)) * 4;
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(kSimtThreads, tree_simt_ctas(HD, L)) k_tree_si
 }
 
 // ---- CUDA cores: any head_dim and alignment, fp32 ----------------------------------------------------------
-// The kernel for what the others do not take, 3 times slower than k_tree_simt_hd on the same case.
+// The kernel for what the others do not take (64 rows of 4 heads a group, 4 x 2064 keys of 4 heads, fp32, head_dim 96: 940 us).
 // grid (stretch, kv head, sequence * line tiles); 4 warps of 4 lines.  Scores: a lane takes a key; products with V: a lane
 // takes dims.
 constexpr int kTreeLines = 16, kTreeKeys = 32;
