@@ -28,9 +28,9 @@
 //
 // Why N = 32, 64 or 128: a column costs softmax time whether it has a line or not, and every further unit streams the keys again.
 // 32 lines and e4m3 leave room for two CTAs on an SM, whose starts and softmax overlap.  128 lines take in 64 KB of bf16 a tile for
-// four times as many as 32: 4 x 4000 keys, 128 rows of 7 heads 52 us, with 64 lines 67.  Over e4m3 a line costs about the same in all
-// three (0.89 us a tile of 64 lines with 128, 1.06 with 64, 1.1 with 32): there the softmax bounds (12 x 4635 keys of 8 heads, 121 rows
-// of 4 heads a group 221 us, 144 with half the heads).  Which one is taken: kCost8, kCost16 (tree_attn.cu).
+// four times as many as 32: 4 x 4000 keys, 128 rows of 7 heads 52 us, with 64 lines 67.  Over e4m3 the
+// softmax bounds: a tile of 64 lines takes 0.73 us of 128, 0.97 alone, 1.1 as two of 32 (12 x 4635 keys of 8 heads, 121 rows of 4 heads a
+// group 190 us, 128 with half the heads).  Which one is taken: kCost8, kCost16 (tree_attn.cu).
 //
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
@@ -51,6 +51,10 @@ struct TreeTc {
   static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : (Q8 ? 3 : 2);
   static constexpr int kP = Q8 && N >= 64 ? 2 : 1;             // tiles of P: with two no warp waits for the product before
   static constexpr int kRingV = N == 32 ? 3 : kRingK;
+  // Half of the softmax warps turn scores into P while the other half reads and scales its scores: left alone all warps do the
+  // same at the same time, and the unit for 2^x is idle for the rest (a tile of 128 x 128 1.80 -> 1.46 us, 64 lines 1.07 -> 0.97; with
+  // 128 lines over bf16 1.25 -> 1.68)
+  static constexpr bool kTurns = Q8 && N >= 64;
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
   static constexpr int kCtl = ((N == 128 ? 5 : 3) + (Q8 ? 4 : 0)) * 1024;
@@ -66,7 +70,7 @@ constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.8f, kAhead = 1.f;
 
 template <int N, bool Q8>
 struct TreeCtl {
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full[2], p_empty[2];
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full[2], p_empty[2], turn[2];   // turn: a half is done with 2^x
   uint32_t tmem_base;
   int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
@@ -356,6 +360,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], Q8 ? 2 : 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
     for (int i = 0; i < C::kP; ++i) { ptx::mbar_init(&c.p_full[i], 4 * C::kGroups); ptx::mbar_init(&c.p_empty[i], 1); }   // (full: the softmax warps)
+    for (int i = 0; i < 2; ++i) ptx::mbar_init(&c.turn[i], 2 * C::kGroups);
     ptx::fence_barrier_init();
     ptx::fence_proxy_async_smem();
   }
@@ -673,6 +678,11 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         else st16(p_piece(q, 1) + p_at, h[4], h[5], h[6], h[7]);
       };
       // the P before in this place has been read (a warp whose wait ran out goes on to the next barrier of its group)
+      if (C::kTurns) {       // (a half's tile j is behind the other's tile j or j - 1)
+        const int team = group * 2 / C::kGroups;
+        if (team == 1 || j > 0) ok = tree_wait_warp(&c.turn[team ^ 1], (uint32_t)(j + team - 1) & 1u, abort_flag);
+        if (!ok) continue;
+      }
       if (C::kP == 2) {
         if (j > 1) ok = tree_wait_warp(&c.p_empty[j & 1], (uint32_t)((j - 2) >> 1) & 1u, abort_flag);
         if (!ok) continue;
@@ -706,6 +716,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&c.p_full[j % C::kP]);
+      if (C::kTurns && lane == 0) ptx::mbar_arrive(&c.turn[group * 2 / C::kGroups]);
     }
     // O^T is complete once the last P has been read
     if (ok) ok = tree_wait_warp(&c.p_empty[(T - 1) % C::kP], (uint32_t)((T - 1) / C::kP) & 1u, abort_flag);

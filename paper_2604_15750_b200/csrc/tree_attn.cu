@@ -82,7 +82,7 @@ struct TreePlan {
 // queries, the first loads' way, the output), with every place of the SMs taken and with one unit an SM; and what it takes more as a
 // CTA of a cluster
 struct TreeCost { int lines, resident, tile, rest, tile_alone, rest_alone, cluster; };
-constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 106, 460, 106, 460, 350}, {128, 1, 176, 700, 176, 700, 500}};
+constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 97, 470, 97, 470, 350}, {128, 1, 146, 790, 146, 790, 500}};
 constexpr TreeCost kCost16[3] = {{32, 1, 67, 250, 67, 250, 100}, {64, 1, 74, 350, 74, 350, 350}, {128, 1, 128, 660, 128, 660, 500}};
 constexpr TreeCost kCost64[3] = {{8, 3, 870, 30, 760, 30, 0}, {32, 2, 980, 230, 950, 200, 0}, {64, 2, 1744, 610, 1680, 570, 0}};    // k_tree_simt_hd
 constexpr TreeCost kCost128[3] = {{8, 3, 1640, 50, 1430, 30, 0}, {32, 2, 1820, 420, 1750, 390, 0}, {64, 1, 2535, 770, 2535, 770, 0}};
