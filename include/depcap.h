@@ -521,7 +521,9 @@ DC_API int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream);
  * Query head h uses kv head h / (n_q_heads / n_kv_heads).  What the cache holds at other keys does not matter, NaN included;
  * a row that sees a drafted key whose V has a value that is not finite becomes NaN in that dim at least, one that does not
  * see it is not touched by it.  Sums and softmax in fp32.  On the tensor cores (bf16 rows, head_dim 128, cache of bf16 or e4m3, arrays
- * on 16-byte boundaries) probabilities are rounded to 8 significant bits, as bf16 has. */
+ * on 16-byte boundaries) probabilities are rounded to 8 significant bits, as bf16 has.  Over an e4m3 cache, there: a key's probability x
+ * scale of V is held to 2^-27 of the largest among 2^17 keys or fewer, if that is more than its 8 bits; a scale of V below 2^-100 counts
+ * as 2^-100; and the scales of V lie within 2^120 of one another (dc_cache_write's do, where all of V is below 2^48). */
 typedef struct dc_tree_in {
   int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
   int32_t layer;          /* of the cache                                                   */

@@ -8,13 +8,17 @@
 // Few lines stream many keys: the cache's bytes are the bound (64 KB of bf16 or 32 KB of e4m3 a tile of 128 keys; at
 // 6.5 TB/s an SM gets one in 2800 or 1400 clocks), and one thread per key does the softmax of N lines in less.
 //
-// An e4m3 cache goes to the tensor cores as it is (kind::f8f6f4), no byte of it is converted.  The other operand must be
-// e4m3 too, and one e4m3 number has 4 significant bits, so it is given as the sum of two:
+// An e4m3 cache goes to the tensor cores as it is (kind::f8f6f4), no byte of it is converted.  The other operand must have 8 bits
+// too, and one such number has 3 or 4 significant bits, so it is given as a sum:
 //   q = 2^e (hi + lo): 4 + 4 bits hold the 8 of a bf16 value exactly (per line, largest magnitude in [128, 256); what is
 //     2^10 below that is off by 2^-18 of it at most); both products go to the same accumulator
-//   P' = 2^(t + log2 v_scale + 4 - m) = hi + lo / 16: 8 bits, not finer than 2^-14 where the largest is 8 .. 446; two accumulators
+//   P' = 2^(t + log2 v_scale + 11 - m) = three e5m2, whose exponents are those of fp16: the upper byte of the fp16 pattern, that of what
+//     is left, and of what is left then the nearest: off by 2^-9 of the value, or 2^-17 where that is more, and the largest is
+//     2^10 .. 2^15.8.  So keys count down to 2^-27 of a line's largest p v_scale, and 2^17 of them (a stretch has no more:
+//     kTreeMostTiles) lose 2^-10 of it at most.  (Two e4m3 parts ended at 2^-17 of it while the sum still counted them: 16000
+//     equal keys 2^-17 below one key lost a quarter of what they add.)
 // The scales are factors of a key, and a thread has one key: K's goes into t, V's into P', so that the sum of a line
-// takes P' / (16 v_scale).  The maximum m is that of t + log2 v_scale.
+// takes P' / (2^11 v_scale).  The maximum m is that of t + log2 v_scale.
 //
 // m of a line is about the maximum of the first tile that it sees and moves only when a later tile has a t far above it
 // (a vote of the four warps that hold a line's keys): then O and the sums are scaled by 2^(m_old - m_new).
@@ -48,25 +52,27 @@ struct TreeTc {
   static constexpr int kGroups = N / kLines, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
   // slots of the rings, as shared memory has room
-  static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : (Q8 ? 3 : 2);
+  static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : 2;
   static constexpr int kP = Q8 && N >= 64 ? 2 : 1;             // tiles of P: with two no warp waits for the product before
-  static constexpr int kRingV = N == 32 ? 3 : kRingK;
+  static constexpr int kRingV = N == 32 || (Q8 && N == 128) ? 3 : kRingK;
   // Half of the softmax warps turn scores into P while the other half reads and scales its scores: left alone all warps do the
   // same at the same time, and the unit for 2^x is idle for the rest (a tile of 128 x 128 1.80 -> 1.46 us, 64 lines 1.07 -> 0.97; with
   // 128 lines over bf16 1.25 -> 1.68)
   static constexpr bool kTurns = Q8 && N >= 64;
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
-  static constexpr int kOperand = N * 256;                     // bytes of Q, and of P
+  static constexpr int kOperand = N * 256;                     // bytes of Q
+  static constexpr int kPTile = (Q8 ? 3 : 2) * N * 128;        // bytes of P: three parts, or bf16
   static constexpr int kCtl = ((N == 128 ? 5 : 3) + (Q8 ? 4 : 0)) * 1024;
-  static constexpr int kSmem = (1 + kP) * kOperand + (kRingK + kRingV) * kSlot + kCtl;
+  static constexpr int kSmem = kOperand + kP * kPTile + (kRingK + kRingV) * kSlot + kCtl;
   // P: the rows of the keys, of 128 bytes at most; a second half of the lines lies behind (bf16, 128 lines)
   static constexpr int kPRow = Q8 ? N : N == 128 ? 128 : 2 * N;
-  static constexpr int kColO = 2 * N, kCols = Q8 ? 4 * N : N == 32 ? 128 : N == 64 ? 256 : 512;   // TMEM: S^T twice, O^T (its two parts)
-  static_assert(kColO + (Q8 ? 2 : 1) * N <= kCols && kSmem <= 232448, "TMEM, shared memory");
+  static constexpr int kColO = 2 * N, kCols = N == 32 ? 128 : N == 64 ? 256 : 512;   // TMEM: S^T twice, O^T
+  static_assert(kColO + N <= kCols && kSmem <= 232448 && kResident * (kSmem + 1024) <= 233472, "TMEM, shared memory");
+  static_assert(N * 512 <= kOperand + kP * kPTile, "the output of a stretch in fp32 lies where Q and P were");
 };
-// P' of e4m3 is 2^8.8 at most (e4m3 ends at 448): m is set 1 above the maximum, which leaves 5.8 for later tiles, and each time that
-// m moves costs about half a tile.
-constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 8.8f, kAhead = 1.f;
+// P' over e4m3 is 2^15.8 at most (e5m2 ends at 1.75 x 2^15): m is set 1 above the maximum, where P' is 2^11, which leaves 5.8 for later
+// tiles, and each time that m moves costs about half a tile.
+constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 15.8f, kAhead = 1.f, kUp = 11.f;
 
 template <int N, bool Q8>
 struct TreeCtl {
@@ -143,10 +149,10 @@ __device__ __forceinline__ void tree_umma(uint32_t d, uint32_t a_lo, uint32_t a_
         "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
         ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
-// 128 x n, fp32 sums; B with its rows (N) or with its columns (the depth) as the contiguous axis
+// 128 x n, fp32 sums; B with its rows (N) or with its columns (the depth) as the contiguous axis; over e4m3 B is e4m3 or e5m2
 template <bool Q8>
-__device__ __forceinline__ uint32_t tree_idesc(int n, bool rows_contiguous) {
-  return (1u << 4) | (Q8 ? 0u : (1u << 7) | (1u << 10)) | (rows_contiguous ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+__device__ __forceinline__ uint32_t tree_idesc(int n, bool rows_contiguous, bool e5m2) {
+  return (1u << 4) | (Q8 ? (e5m2 ? 1u << 10 : 0u) : (1u << 7) | (1u << 10)) | (rows_contiguous ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 // Upper half of the descriptor of P: rows (keys) of `row` bytes = one swizzle span, 8 of them a group
 __device__ __forceinline__ uint32_t tree_p_desc_hi(int row) {
@@ -156,20 +162,20 @@ __device__ __forceinline__ uint32_t tree_p_desc_hi(int row) {
 __device__ __forceinline__ uint32_t tree_e4m3x2(float x0, float x1) {
   return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
 }
-// Four values, two in an f16x2, as hi + lo / 16 of e4m3: hi rounded, lo of 16 times the rest
-__device__ __forceinline__ void tree_split4(__half2 x, __half2 y, uint32_t& hi, uint32_t& lo) {
-  const __half2 m16 = __float2half2_rn(-16.f);
-  const __half2 x16 = __hmul2(x, __float2half2_rn(16.f)), y16 = __hmul2(y, __float2half2_rn(16.f));
-  asm("{\n\t.reg .b16 h0, h1, l0, l1;\n\t.reg .b32 r0, r1;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 h0, %2;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h1, %3;\n\t"
-      "mov.b32 %0, {h0, h1};\n\t"
-      "cvt.rn.f16x2.e4m3x2 r0, h0;\n\tcvt.rn.f16x2.e4m3x2 r1, h1;\n\t"
-      "fma.rn.f16x2 r0, r0, %4, %5;\n\tfma.rn.f16x2 r1, r1, %4, %6;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f16x2 l0, r0;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l1, r1;\n\t"
-      "mov.b32 %1, {l0, l1};\n\t}"
-      : "=r"(hi), "=r"(lo)
-      : "r"(*reinterpret_cast<const uint32_t*>(&x)), "r"(*reinterpret_cast<const uint32_t*>(&y)), "r"(*reinterpret_cast<const uint32_t*>(&m16)),
-        "r"(*reinterpret_cast<const uint32_t*>(&x16)), "r"(*reinterpret_cast<const uint32_t*>(&y16)));
+// Four values >= 0, two in an f16x2, as sums of three e5m2: an e5m2 is the upper byte of an fp16.  (A NaN stays one in the first part.)
+__device__ __forceinline__ __half2 tree_upper(__half2 x) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(&x) & 0xff00ff00u;
+  return *reinterpret_cast<const __half2*>(&w);
+}
+__device__ __forceinline__ uint32_t tree_bytes(__half2 x, __half2 y, uint32_t add) {    // (fp16 patterns are below 2^15: no carry)
+  return __byte_perm(*reinterpret_cast<const uint32_t*>(&x) + add, *reinterpret_cast<const uint32_t*>(&y) + add, 0x7531);
+}
+__device__ __forceinline__ void tree_split4(__half2 x, __half2 y, uint32_t (&part)[3]) {
+  part[0] = tree_bytes(x, y, 0u);
+  x = __hsub2(x, tree_upper(x)); y = __hsub2(y, tree_upper(y));
+  part[1] = tree_bytes(x, y, 0u);
+  x = __hsub2(x, tree_upper(x)); y = __hsub2(y, tree_upper(y));
+  part[2] = tree_bytes(x, y, 0x00800080u);       // (half of what the lower byte can hold: to the nearest)
 }
 __device__ __forceinline__ __half2 tree_half2(uint32_t e4m3x2) {
   return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)e4m3x2, __NV_E4M3));
@@ -211,7 +217,7 @@ __device__ __forceinline__ bool tree_wait_warp(uint64_t* bar, uint32_t parity, v
 }
 __device__ __forceinline__ float tree_rcp(float x) {
   float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float tree_lg2(float x) {
@@ -344,7 +350,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   const int T = min((keys + kTreeTile - 1) / kTreeTile - tile0, a.tiles);
   // (a cluster's barriers wait for the CTAs that are still there, and nobody reads the shared memory of one without keys)
   if (n <= 0 || T <= 0) { pdl_wait(); return; }
-  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kP * C::kOperand, *vring = kring + C::kRingK * C::kSlot;
+  uint8_t *Qs = smem_tree, *Ps = Qs + C::kOperand, *kring = Ps + C::kP * C::kPTile, *vring = kring + C::kRingK * C::kSlot;
   TreeCtl<N, Q8>& c = *reinterpret_cast<TreeCtl<N, Q8>*>(vring + C::kRingV * C::kSlot);
   static_assert(sizeof(TreeCtl<N, Q8>) <= C::kCtl, "control block");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -476,11 +482,11 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   } else if (warp == 1 || warp == 2) {
     // ---------------- issuers of S^T = K Q^T (warp 1) and O^T (+)= V^T P^T (warp 2) ----------------
     const bool pv = warp == 2;
-    const uint32_t idesc = tree_idesc<Q8>(N, pv), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
+    const uint32_t idesc = tree_idesc<Q8>(N, pv, pv), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
     // (two halves of lines lie 128 rows of 128 bytes apart)
     const uint32_t b_lo = pv && !Q8 && N == 128 ? (1024u << 16) | ((ptx::smem_u32(Ps) >> 4) & 0x3fffu) : ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs));
     const uint32_t ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
-    // from one product to the next: Q goes on in its row, P by the rows of 16 (32) keys; hi and lo lie behind one another
+    // from one product to the next: Q goes on in its row, P by the rows of 16 (32) keys; the parts lie behind one another
     const uint32_t b_step = pv ? (uint32_t)((Q8 ? 32 : 16) * C::kPRow >> 4) : 2u, b_half = pv ? 4u * b_step : (uint32_t)(N * 128 >> 4);
     bool ok = true;
     for (int j = 0; j < T && ok; ++j) {
@@ -513,13 +519,15 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         const int nk = pv ? (valid_keys(j) + (Q8 ? 31 : 15)) / (Q8 ? 32 : 16) : Q8 ? 4 : 8;
         if (Q8) {
 #pragma unroll
-          for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < 3; ++part) {
+            if (!pv && part == 2) break;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= nk) break;
-              tree_umma<Q8>(pv ? d + part * N : d, t + kk * 2, a_hi, b_lo + (pv && j % C::kP ? C::kOperand >> 4 : 0) + part * b_half + kk * b_step, b_hi, idesc,
-                            (kk > 0 || (pv ? j > 0 : part > 0)) ? 1u : 0u);
+              tree_umma<Q8>(d, t + kk * 2, a_hi, b_lo + (pv && j % C::kP ? C::kPTile >> 4 : 0) + part * b_half + kk * b_step, b_hi, idesc,
+                            (kk > 0 || part > 0 || (pv && j > 0)) ? 1u : 0u);
             }
+          }
         } else {
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk) {
@@ -541,7 +549,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float v_sc = vs[i] < 7.8886091e-31f ? 7.8886091e-31f : vs[i];   // 2^-100 (a row of zeros may come with a scale of 0: it counts in the sum)
-        f[i] = make_float4(ks[i] * a.scale_log2, tree_lg2(v_sc), v_sc <= 3.402823466e38f ? tree_rcp(v_sc * 16.f) : 0.f, 0.f);
+        f[i] = make_float4(ks[i] * a.scale_log2, tree_lg2(v_sc), v_sc <= 3.402823466e38f ? tree_rcp(v_sc) * 0x1p-11f : 0.f, 0.f);
       }
       if (j + 1 < T) load_scales(j + 1);
       if (j >= 2 && !tree_wait_warp(&c.s_empty[j & 1], ((uint32_t)(j - 2) >> 1) & 1u, abort_flag)) break;
@@ -569,7 +577,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = 0ull;
     // the exponents of P from the scores of 16 lines, -infinity where a line does not see the key
     auto exponents = [&](float (&v)[16], int col, float mul, float lv, uint32_t sees) {
-      const ptx::f32x2 off2 = ptx::f2_pack(lv + 4.f, lv + 4.f), mul2 = ptx::f2_pack(mul, mul);
+      const ptx::f32x2 off2 = ptx::f2_pack(lv + kUp, lv + kUp), mul2 = ptx::f2_pack(mul, mul);
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const ulonglong2 m2 = *reinterpret_cast<const ulonglong2*>(&c.nm[col + i]);
@@ -650,9 +658,9 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           for (int i = 0; i < QN * 8; ++i) acc[i / 8][i % 8] = ptx::f2_mul(acc[i / 8][i % 8], *reinterpret_cast<const ptx::f32x2*>(&c.fac[col0 + 2 * i]));
           ptx::tc_fence_after();
 #pragma unroll 1
-          for (int i = 0; i < (Q8 ? 2 * CW : CW); i += 4) {
-            const uint32_t at = t_lane + (uint32_t)(C::kColO + (i & ~(CW - 1)) / CW * N + (i & (CW - 1)));
-            const float4 f = *reinterpret_cast<const float4*>(&c.fac[col0 + (i & (CW - 1))]);
+          for (int i = 0; i < CW; i += 4) {
+            const uint32_t at = t_lane + (uint32_t)(C::kColO + i);
+            const float4 f = *reinterpret_cast<const float4*>(&c.fac[col0 + i]);
             float o[4];
             tree_tmem_ld4(at, o);
             ptx::tmem_ld_wait();
@@ -670,12 +678,16 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       auto st16 = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
       };
-      uint32_t hi[QN][Q8 ? 4 : 8], lo[QN][Q8 ? 4 : 1];     // bf16: 16 lines; e4m3: 16 lines of each part
-      const uint32_t p_at = C::kP == 2 && (j & 1) ? (uint32_t)C::kOperand : 0u;
-      auto store = [&](int q, const auto& h, const auto& l) {
-        st16(p_piece(q, 0) + p_at, h[0], h[1], h[2], h[3]);
-        if constexpr (Q8) st16(p_piece(q, 0) + p_at + 128 * C::kPRow, l[0], l[1], l[2], l[3]);
-        else st16(p_piece(q, 1) + p_at, h[4], h[5], h[6], h[7]);
+      uint32_t p[QN][4][Q8 ? 3 : 2];     // of 16 lines, four by four: e4m3 the three parts of them, bf16 two words
+      const uint32_t p_at = C::kP == 2 && (j & 1) ? (uint32_t)C::kPTile : 0u;
+      auto store = [&](int q) {
+        if constexpr (Q8) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) st16(p_piece(q, 0) + p_at + i * 128 * C::kPRow, p[q][0][i], p[q][1][i], p[q][2][i], p[q][3][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) st16(p_piece(q, i) + p_at, p[q][2 * i][0], p[q][2 * i][1], p[q][2 * i + 1][0], p[q][2 * i + 1][1]);
+        }
       };
       // the P before in this place has been read (a warp whose wait ran out goes on to the next barrier of its group)
       if (C::kTurns) {       // (a half's tile j is behind the other's tile j or j - 1)
@@ -697,21 +709,21 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
             acc[q][i / 2] = ptx::f2_add(acc[q][i / 2], ptx::f2_pack(p0, p1));
             acc[q][i / 2 + 1] = ptx::f2_add(acc[q][i / 2 + 1], ptx::f2_pack(p2, p3));
             const __nv_bfloat162 w0 = __floats2bfloat162_rn(p0, p1), w1 = __floats2bfloat162_rn(p2, p3);
-            hi[q][i / 2] = *reinterpret_cast<const uint32_t*>(&w0);
-            hi[q][i / 2 + 1] = *reinterpret_cast<const uint32_t*>(&w1);
+            p[q][i / 4][0] = *reinterpret_cast<const uint32_t*>(&w0);
+            p[q][i / 4][1] = *reinterpret_cast<const uint32_t*>(&w1);
           } else {
             acc[q][i / 2] = ptx::f2_fma(ptx::f2_pack(p0, p1), iv2, acc[q][i / 2]);
             acc[q][i / 2 + 1] = ptx::f2_fma(ptx::f2_pack(p2, p3), iv2, acc[q][i / 2 + 1]);
-            tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), hi[q][i / 4], lo[q][i / 4]);
+            tree_split4(__floats2half2_rn(p0, p1), __floats2half2_rn(p2, p3), p[q][i / 4]);
           }
         }
-        if (C::kP == 2) store(q, hi[q], lo[q]);
+        if (C::kP == 2) store(q);
       }
       if (C::kP == 1) {
         if (j > 0) ok = tree_wait_warp(&c.p_empty[0], (uint32_t)(j - 1) & 1u, abort_flag);
         if (!ok) continue;
 #pragma unroll
-        for (int q = 0; q < QN; ++q) store(q, hi[q], lo[q]);
+        for (int q = 0; q < QN; ++q) store(q);
       }
       ptx::fence_proxy_async_smem();
       __syncwarp();
@@ -756,15 +768,14 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     ptx::tc_fence_after();
 #pragma unroll 1
     for (int i = 0; i < ng; i += 4) {
-      float o[4], lo[4];
+      float o[4];
       tree_tmem_ld4(o_col + i, o);        // (whatever is there after a wait that ran out: l is NaN)
-      if (Q8) tree_tmem_ld4(o_col + N + i, lo);
       ptx::tmem_ld_wait();
       const float4 f = *reinterpret_cast<const float4*>(&c.fac[col0 + i]);
       const float ff[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (Q8) o[e] = fmaf(lo[e], 1.f / 16.f, o[e]) * (1.f / 16.f);
+        if (Q8) o[e] *= 0x1p-11f;
         o[e] = ff[e] == 0.f ? 0.f : o[e] * ff[e];
         if (alone) reinterpret_cast<__nv_bfloat16*>(smem_tree)[(col0 + i + e) * kHd + dim] = __float2bfloat16_rn(o[e]);
         else reinterpret_cast<float*>(smem_tree)[(col0 + i + e) * kHd + dim] = o[e];

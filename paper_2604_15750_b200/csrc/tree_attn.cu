@@ -124,7 +124,9 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, T
     const long long cost = n / slots * two + last, most = t * k.tile_alone + k.rest_alone + more;
     return cost > most ? cost : most;
   };
-  for (int s = 1, before = 0; s <= longest && s <= 256; ++s) {
+  // (an 8-bit cache's probabilities end 2^-27 below the largest of a stretch: tc_tree.cuh)
+  const int fewest = kind == TreePlan::kTc && c->dtype == DC_E4M3 ? (longest + kTreeMostTiles - 1) / kTreeMostTiles : 1;
+  for (int s = fewest < 1 ? 1 : fewest, before = 0; s <= longest && (s <= 256 || p.cost < 0); ++s) {
     const int t = (longest + s - 1) / s;
     if (t == before) continue;
     before = t;

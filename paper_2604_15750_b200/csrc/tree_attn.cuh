@@ -12,6 +12,7 @@
 namespace dc {
 
 constexpr int kTreeTile = 128;   // keys: stretches are whole tiles
+constexpr int kTreeMostTiles = 1024;     // of a stretch over an 8-bit cache on the tensor cores (tc_tree.cuh)
 
 struct TreeArgs {
   dc_cache c;                    // k, v, scales moved to the layer
