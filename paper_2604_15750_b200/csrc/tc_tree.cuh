@@ -10,8 +10,9 @@
 //
 // An e4m3 cache goes to the tensor cores as it is (kind::f8f6f4), no byte of it is converted.  The other operand must have 8 bits
 // too, and one such number has 3 or 4 significant bits, so it is given as a sum:
-//   q = 2^e (hi + lo): 4 + 4 bits hold the 8 of a bf16 value exactly (per line, largest magnitude in [128, 256); what is
-//     2^10 below that is off by 2^-18 of it at most); both products go to the same accumulator
+//   q = 2^e (hi + lo), e4m3 and e5m2, per line with the largest magnitude in [128, 256): hi leaves at most 8 units of a bf16 value's
+//     last place, whole ones, which 3 bits hold, so down to 2^-13 of the largest every value is exact; what is below is off by
+//     2^-14, 2^-21 of the largest, at most (lo as e4m3: 2^-9 and 2^-17); both products go to the same accumulator
 //   P' = 2^(t + log2 v_scale + 11 - m) = three e5m2, whose exponents are those of fp16: the upper byte of the fp16 pattern, that of what
 //     is left, and of what is left then the nearest: off by 2^-9 of the value, or 2^-17 where that is more, and the largest is
 //     2^10 .. 2^15.8.  So keys count down to 2^-27 of a line's largest p v_scale, and 2^17 of them (a stretch has no more:
@@ -159,8 +160,8 @@ __device__ __forceinline__ uint32_t tree_p_desc_hi(int row) {
   return (uint32_t)(8 * row >> 4) | (1u << 14) | ((row == 128 ? 2u : row == 64 ? 4u : 6u) << 29);
 }
 
-__device__ __forceinline__ uint32_t tree_e4m3x2(float x0, float x1) {
-  return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, __NV_E4M3);
+__device__ __forceinline__ uint32_t tree_fp8x2(float x0, float x1, __nv_fp8_interpretation_t as) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(x0, x1), __NV_SATFINITE, as);
 }
 // Four values >= 0, two in an f16x2, as sums of three e5m2: an e5m2 is the upper byte of an fp16.  (A NaN stays one in the first part.)
 __device__ __forceinline__ __half2 tree_upper(__half2 x) {
@@ -262,10 +263,10 @@ __device__ __forceinline__ void tree_store_q(int item, const uint4& v, uint8_t* 
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float x0 = __uint_as_float(w[e] << 16) * f, x1 = __uint_as_float(w[e] & 0xffff0000u) * f;
-    const uint32_t h = tree_e4m3x2(x0, x1);
+    const uint32_t h = tree_fp8x2(x0, x1, __NV_E4M3);
     const float2 r = __half22float2(tree_half2(h));
     hi[e >> 1] |= h << (16 * (e & 1));
-    lo[e >> 1] |= tree_e4m3x2(x0 - r.x, x1 - r.y) << (16 * (e & 1));
+    lo[e >> 1] |= tree_fp8x2(x0 - r.x, x1 - r.y, __NV_E5M2) << (16 * (e & 1));
   }
   uint8_t* at = Qs + line * 128 + (((c >> 1) ^ (line & 7)) << 4) + (c & 1) * 8;
   *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
@@ -482,7 +483,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   } else if (warp == 1 || warp == 2) {
     // ---------------- issuers of S^T = K Q^T (warp 1) and O^T (+)= V^T P^T (warp 2) ----------------
     const bool pv = warp == 2;
-    const uint32_t idesc = tree_idesc<Q8>(N, pv, pv), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
+    const uint32_t idesc = tree_idesc<Q8>(N, pv, pv), idesc_lo = tree_idesc<Q8>(N, pv, true), a_hi = ptx::smem_desc_hi32(), b_hi = pv ? tree_p_desc_hi(C::kPRow) : a_hi;
     // (two halves of lines lie 128 rows of 128 bytes apart)
     const uint32_t b_lo = pv && !Q8 && N == 128 ? (1024u << 16) | ((ptx::smem_u32(Ps) >> 4) & 0x3fffu) : ptx::smem_desc_lo(ptx::smem_u32(pv ? Ps : Qs));
     const uint32_t ring_lo = ptx::smem_desc_lo(ptx::smem_u32(pv ? vring : kring));
@@ -524,7 +525,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               if (kk >= nk) break;
-              tree_umma<Q8>(d, t + kk * 2, a_hi, b_lo + (pv && j % C::kP ? C::kPTile >> 4 : 0) + part * b_half + kk * b_step, b_hi, idesc,
+              tree_umma<Q8>(d, t + kk * 2, a_hi, b_lo + (pv && j % C::kP ? C::kPTile >> 4 : 0) + part * b_half + kk * b_step, b_hi, part ? idesc_lo : idesc,
                             (kk > 0 || part > 0 || (pv && j > 0)) ? 1u : 0u);
             }
           }

@@ -59,3 +59,29 @@ def test_a_flat_tail_far_below_one_key_counts(rows, B, H, keys, below, first):
     assert torch.equal(out, out[:1, :, :1].expand_as(out))
     over = (out[0, :, :1].double().cpu() - o).abs() / tol
     assert (over <= 1).all(), float(over.max())
+
+
+@pytest.mark.parametrize("rows", [8, 64, 128])
+def test_small_dims_of_a_query_beside_a_large_one_are_exact(rows):
+    """A query's dims down to 2^-13 of its largest one are held exactly, as sums of two 8-bit numbers: half of the keys have the dims
+    with x = 2^-10 (1 + 2^-7) of the largest, half those with 2^-10 of it, and only what x has more decides between them."""
+    keys, scale = 512, 128 ** -0.5
+    q = torch.zeros((rows, 128))
+    q[:, 0], q[:, 1:64], q[:, 64:127] = 2.0 ** 13, 8 * (1 + 2.0 ** -7), 8
+    sign = torch.randint(0, 2, (rows, 1), generator=torch.Generator().manual_seed(1)) * 2 - 1
+    q = (q * sign).to(BF16)
+    k = torch.zeros((keys, 128))
+    k[0::2, 1:64] = k[1::2, 64:127] = 1
+    v = torch.ones((keys, 128))
+    v[1::2] = -1
+    c = dc.KvCache.empty(1, 1, 1, keys, 128, E4M3, DEV)
+    shape = lambda t: t.to(BF16).to(DEV)[None, :, None]
+    dc.cache_write(c, shape(k), shape(v), [0])
+    out = dc.tree_attention(shape(q).contiguous(), c, [keys - rows], [rows])[0].double().cpu()
+    kk = c.k[0, 0].double().cpu() * c.k_scale[0, 0].double().cpu()[..., None]
+    v8, vs = c.v[0, 0].float().cpu().transpose(1, 2), c.v_scale[0, 0].cpu()
+    p = torch.softmax(q.double() @ kk[0].T * scale, -1)
+    o = (p @ (v8[0].double() * vs[0].double()[:, None]))[:, None]
+    assert float(o.abs().min()) > 0.15
+    over = (out - o).abs() / _tolerance(q[:, None], kk, v8, vs, p[None], o, scale)
+    assert (over <= 1).all(), float(over.max())
