@@ -434,6 +434,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   static_assert(N <= 128, "a thread a line");
   if (threadIdx.x < N) c.nm[threadIdx.x] = (int)threadIdx.x < n ? INFINITY : -INFINITY;   // (columns without a line: P = 0)
   if (warp == 1) {
+    __syncwarp();
     ptx::tmem_alloc(&c.tmem_base, C::kCols);
     ptx::tmem_relinquish();
   }
@@ -641,6 +642,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
             u[e] = tree_max((sees >> (i + e)) & 1u ? u[e] : -INFINITY);
           }
           if (lane == 0) *reinterpret_cast<float4*>(&c.part[quarter][col0 + i]) = make_float4(u[0], u[1], u[2], u[3]);
+          __syncwarp();
         }
         if (j > 0)   // O^T: all products so far are in
           ok = ok && tree_wait_warp(&c.p_empty[(j - 1) % C::kP], (uint32_t)((j - 1) / C::kP) & 1u, abort_flag);
@@ -653,6 +655,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
           c.nm[col] = -now;                            // (of columns without a line it stays infinite)
           c.fac[col] = old == -INFINITY ? 0.f : attn_ex2(old - now);
         }
+        __syncwarp();
         asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory");
         if (j > 0) {
 #pragma unroll
@@ -796,6 +799,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   }
   if (a.cluster) {
     // the stretches of these lines are the CTAs of the cluster: each joins some of the lines, a warp a line, from the others' shared memory
+    // (the barriers want whole warps, and the rows above end inside one)
+    __syncwarp();
     ptx::cluster_sync();
     if (!alone) {
       for (int line = (int)blockIdx.x + warp * stretches; line < n; line += C::kThreads / 32 * stretches) {
@@ -825,6 +830,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
         }
       }
     }
+    __syncwarp();
     ptx::cluster_sync();      // nobody leaves while another reads its shared memory
   }
   if (loads_k > 0 && c.abort_flag != 0) {
