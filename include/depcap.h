@@ -361,8 +361,12 @@ DC_API int dc_generate(dc_ctx* ctx, const dc_generate_in* in, const dc_generate_
  *     out: the step then ends with DC_ERR_TIMEOUT in every status[b] and the context stays usable.
  *   DC_OPT_TEST_STALL_STEP (default 0): the same for the fused CUDA-core step.  1 makes one of its CTAs leave
  *     at once, so that the grid barrier of the others runs out.
+ *   DC_OPT_TEST_STALL_TREE (default 0): the same for dc_tree_attention on the tensor cores, of the whole process.  1: no CTA
+ *     asks for a tile of keys; 2: for its first one only; 3: those of a sequence's second stretch ask for none.  The rows
+ *     concerned become NaN and the call's status DC_ERR_TIMEOUT.
  * Returns DC_ERR_INVALID_ARG for an unknown option or a value out of range. */
-enum { DC_OPT_COOPERATIVE = 1, DC_OPT_WAIT_LIMIT_US = 2, DC_OPT_TEST_STALL_LMHEAD = 3, DC_OPT_TEST_STALL_STEP = 4 };
+enum { DC_OPT_COOPERATIVE = 1, DC_OPT_WAIT_LIMIT_US = 2, DC_OPT_TEST_STALL_LMHEAD = 3, DC_OPT_TEST_STALL_STEP = 4,
+       DC_OPT_TEST_STALL_TREE = 5 };
 DC_API int dc_set_option(dc_ctx* ctx, int32_t option, int32_t value);
 
 /* Frees the workspace.  The caller must have synchronised the stream.  Null is a no-op. */

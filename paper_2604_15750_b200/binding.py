@@ -24,6 +24,7 @@ EXPORTS = ["dc_create", "dc_step", "dc_boundary", "dc_select", "dc_destroy", "dc
            "dc_set_option", "dc_boundary_batched", "dc_select_batched", "dc_cache_write", "dc_cache_read",
            "dc_qk_norm_rope", "dc_tree_attention", "dc_tree_attention_workspace", "dc_tree_mask"]
 DC_OPT_COOPERATIVE, DC_OPT_WAIT_LIMIT_US, DC_OPT_TEST_STALL_LMHEAD, DC_OPT_TEST_STALL_STEP = 1, 2, 3, 4
+DC_OPT_TEST_STALL_TREE = 5
 
 
 class DepCapError(RuntimeError):

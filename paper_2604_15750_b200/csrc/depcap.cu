@@ -953,6 +953,11 @@ int dc_set_option(dc_ctx* c, int32_t option, int32_t value) {
     c->stall_step = value != 0;
     return DC_OK;
   }
+  if (option == DC_OPT_TEST_STALL_TREE) {
+    if (value < 0 || value > 3) return fail(c, DC_ERR_INVALID_ARG, "DC_OPT_TEST_STALL_TREE outside [0, 3]");
+    tree_set_stall(value);
+    return DC_OK;
+  }
   return fail(c, DC_ERR_INVALID_ARG, "unknown option %d", option);
 }
 

@@ -63,6 +63,7 @@ inline bool op_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 
 // DC_OPT_WAIT_LIMIT_US for the waits of dc_tree_attention's kernel; 0 or a CUDA error
 int tree_set_wait_limit_us(long long us, cudaStream_t s);
+void tree_set_stall(int how);      // DC_OPT_TEST_STALL_TREE
 
 // ---- types --------------------------------------------------------------------------------------------
 __device__ __forceinline__ float op_f32(float x) { return x; }

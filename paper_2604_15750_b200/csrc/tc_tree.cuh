@@ -78,6 +78,7 @@ constexpr float kHeadBf16 = 40.f, kHeadE4m3 = 15.8f, kAhead = 1.f, kUp = 11.f;
 template <int N, bool Q8>
 struct TreeCtl {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], s_empty[2], p_full[2], p_empty[2], turn[2];   // turn: a half is done with 2^x
+  uint64_t ended[2];                     // given up: the issuers' products
   uint32_t tmem_base;
   int abort_flag, late_flag, poisoned;
   uint32_t poison[8];                    // drafted keys whose V is not finite
@@ -367,7 +368,7 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     for (int i = 0; i < C::kRingV; ++i) { ptx::mbar_init(&c.v_full[i], 1); ptx::mbar_init(&c.v_empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.s_full[i], Q8 ? 2 : 1); ptx::mbar_init(&c.s_empty[i], 4 * C::kGroups); }
     for (int i = 0; i < C::kP; ++i) { ptx::mbar_init(&c.p_full[i], 4 * C::kGroups); ptx::mbar_init(&c.p_empty[i], 1); }   // (full: the softmax warps)
-    for (int i = 0; i < 2; ++i) ptx::mbar_init(&c.turn[i], 2 * C::kGroups);
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(&c.turn[i], 2 * C::kGroups); ptx::mbar_init(&c.ended[i], 1); }
     ptx::fence_barrier_init();
     ptx::fence_proxy_async_smem();
   }
@@ -424,7 +425,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
     ptx::tma_load_2d(dst, &map_v, &c.v_full[s], key, vrow);
     if (!Q8) ptx::tma_load_2d(dst + kSub, &map_v, &c.v_full[s], key + 64, vrow);
   };
-  if (threadIdx.x == 0) {
+  const bool silent = a.stall == 1 || (a.stall == 3 && blockIdx.x == 1);     // (test hook: this CTA asks for no tile)
+  if (threadIdx.x == 0 && !silent) {
     // the first tiles are on their way while the CTA sets up, and only these: the others would be in the way of the queries of the
     // CTAs that start later (8 x 1200 keys, 24 rows: the whole rings 22.6 us, one K tile 21.4, one of each 21.2)
     load_k(0);
@@ -469,8 +471,8 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer ----------------
-      loads_k = loads_v = 1;
-      while (loads_k < T || loads_v < T) {
+      loads_k = loads_v = silent ? 0 : 1;
+      while (!silent && a.stall != 2 && (loads_k < T || loads_v < T)) {
         if (loads_k < T) {
           if (loads_k >= C::kRingK && !tree_wait(&c.k_empty[loads_k % C::kRingK], ((uint32_t)(loads_k / C::kRingK) & 1u) ^ 1u, abort_flag)) break;
           load_k(loads_k++);
@@ -839,6 +841,13 @@ k_tree_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUt
       tree_wait(&c.k_full[j % C::kRingK], (uint32_t)(j / C::kRingK) & 1u, &c.late_flag);
     for (int j = max(0, loads_v - C::kRingV); j < loads_v; ++j)
       tree_wait(&c.v_full[j % C::kRingV], (uint32_t)(j / C::kRingV) & 1u, &c.late_flag);
+  }
+  if (c.abort_flag != 0 && (warp == 1 || warp == 2)) {
+    // ... and what was issued ends before the TMEM that it writes, the shared memory that it reads and the barriers that it arrives on go
+    __syncwarp();
+    if (ptx::elect_one()) ptx::umma_commit(&c.ended[warp - 1]);
+    __syncwarp();
+    tree_wait_warp(&c.ended[warp - 1], 0, &c.late_flag);
   }
   ptx::tc_fence_before();
   __syncthreads();

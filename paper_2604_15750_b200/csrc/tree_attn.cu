@@ -245,7 +245,11 @@ bool launch_tc(const TreeArgs& a, const TreePlan& p, int batch, int vec_q, int v
   return cudaLaunchKernelEx(&cfg, k_tree_tc<N, Q8>, mk, mv, a, vec_q, vec_o) == cudaSuccess;
 }
 
+std::atomic<int> tree_stall;      // DC_OPT_TEST_STALL_TREE
+
 }  // namespace
+
+void tree_set_stall(int how) { tree_stall.store(how, std::memory_order_relaxed); }
 
 int tree_set_wait_limit_us(long long us, cudaStream_t s) {
   const unsigned long long ns = (unsigned long long)us * 1000ull;
@@ -296,7 +300,7 @@ extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, vo
   const uint64_t n = (uint64_t)p.joined * p.lines;
   a.part_ml = static_cast<float2*>(in->workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(in->workspace) + n * 8 + (n & 1) * 8);
-  a.status = in->status;
+  a.status = in->status; a.stall = tree_stall.load(std::memory_order_relaxed);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   const bool f32 = in->dtype == DC_F32, q8 = cache->dtype == DC_E4M3;
   const int n_lines = p.kind == TreePlan::kTc ? p.shape : 0;

@@ -33,6 +33,7 @@ struct TreeArgs {
   float* part_o;                 // [stretch][line][head_dim]: sums not divided by l
   float2* part_ml;               // [stretch][line]: maximum (log2 units) and sum
   int32_t* status;
+  int stall;                     // DC_OPT_TEST_STALL_TREE
 };
 
 __device__ __forceinline__ int tree_stretches(const TreeArgs& a, int b) {

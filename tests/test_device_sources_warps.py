@@ -32,3 +32,16 @@ def test_lanes_are_together_at_the_next_read_of_tmem_behind_what_one_lane_does()
     loop = body[body.index("tree_tmem_ld4(s_col + i, u);"):]
     loop = loop[:loop.index("if (j > 0)")]
     assert re.search(r"if \(lane == 0\) \*reinterpret_cast<float4\*>[^;]*;\s*__syncwarp\(\);\s*\}", loop)
+
+
+def test_products_that_were_issued_end_before_a_cta_that_gives_up_leaves():
+    """A commit behind everything that an issuer has issued, and a wait for it with a limit of its own, between the barrier that all roles
+    come to after their last wait and the release of TMEM."""
+    body = _body()
+    ended = body.index("umma_commit(&c.ended")
+    start = body.rindex("if (c.abort_flag != 0", 0, ended)
+    wait = body.index("tree_wait_warp(&c.ended", ended)
+    assert "warp == 1 || warp == 2" in body[start:ended] and "late_flag" in body[wait:body.index(";", wait)]
+    last_role_wait = body.rindex(", abort_flag)", 0, start)
+    assert "__syncthreads();" in body[last_role_wait:start]
+    assert wait < body.rindex("__syncthreads();", 0, body.index("tmem_dealloc("))
