@@ -62,13 +62,18 @@ def _elsewhere(device, *tensors):
             raise ValueError(f"a tensor is on {t.device}, another on {device}")
 
 
+def _on_cuda(index):
+    if index < 0:
+        raise RuntimeError("the operators need tensors on a CUDA device; there is no CPU path")
+
+
 _current, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _call(f, index, stream, *args):
     """f(*args, stream) with device `index` current (-1: not a CUDA device)"""
     if index < 0:
-        raise RuntimeError("the operators need tensors on a CUDA device; there is no CPU path")
+        _on_cuda(index)
     raw = _stream_of(index) if stream is None else stream.cuda_stream
     if index == _current():
         rc = f(*args, raw)
@@ -154,6 +159,8 @@ def _move(f, cache, k, v, pos, n, layer, stream):
     n_at, n_keep = _lengths([most] * batch if n is None else n, batch, "n")
     if n is not None and max(n_keep.tolist(), default=0) > most:
         raise ValueError(f"n asks for more than the {most} rows given")
+    if 0 in (layers, batch, most):       # nothing to do, and an empty tensor has no address
+        return _on_cuda(index)
     _call(f, index, stream, cache._c, _ROWS.pack(batch, layer, layers, _type(k, "rows"), k.data_ptr(), v.data_ptr(), *k.stride(),
                                                  *v.stride(), at, n_at))
 
@@ -252,6 +259,9 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         _elsewhere(cache.device, q, out, mask, workspace, status)
     ctx, keep = _lengths(ctx_len, batch, "ctx_len")
     n, n_keep = _lengths(n_rows, batch, "n_rows")
+    if batch == 0 or rows == 0:
+        _on_cuda(index)
+        return out
     args = (batch, layer, _type(q, "q"), heads, rows, scale, q.data_ptr(), out.data_ptr(), a, b, h, os_[0], os_[1], os_[2], ctx, n, mask_at)
     st = 0 if status is None else status.data_ptr()
     call = _fn.dc_tree_attention
@@ -281,6 +291,8 @@ def tree_attention_workspace(q, cache, ctx_len, n_rows):
     batch, rows, heads, hd = q.shape
     ctx, keep = _lengths(ctx_len, batch, "ctx_len")
     n, n_keep = _lengths(n_rows, batch, "n_rows")
+    if batch == 0 or rows == 0:
+        return 0
     s = q.stride()
     return _need(cache, _TREE.pack(batch, 0, _type(q, "q"), heads, rows, 0.0, q.data_ptr(), q.data_ptr(), s[0], s[1], s[2], s[0], s[1], s[2],
                                    ctx, n, 0, 0, 0, 0))
