@@ -252,8 +252,8 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         raise ValueError("the workspace is contiguous")
     if scale is None:
         scale = 0.0
-    elif not scale > 0:
-        raise ValueError("scale must be positive")
+    elif not scale >= 2.0 ** -126:        # (what fp32 rounds to 0 would be the default)
+        raise ValueError("scale must be positive, a normal fp32 number")
     if q.get_device() != index or out.get_device() != index or workspace is not None or status is not None or \
             (mask is not None and mask.get_device() != index):
         _elsewhere(cache.device, q, out, mask, workspace, status)

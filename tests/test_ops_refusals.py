@@ -208,3 +208,11 @@ def test_the_binding_refuses():
                      ((h, h, pos), dict(q_out=h[:1].expand(3, 4, 128)))]:
         with pytest.raises(ValueError):
             dc.qk_norm_rope(*args, **kw)
+
+
+@pytest.mark.parametrize("scale", [1e-60, 1e-46, 2.0 ** -127])
+def test_a_scale_that_fp32_does_not_hold_is_refused(scale):
+    """Rounded to 0 it would be taken for the default, 1 / sqrt(head_dim)."""
+    q = torch.zeros((2, 3, 4, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="scale"):
+        dc.tree_attention(q, dc.KvCache(*_kv()), [0, 0], [3, 3], scale=scale)
