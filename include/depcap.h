@@ -538,7 +538,7 @@ typedef struct dc_tree_in {
   const void* q;          /* device; the dims of a head are contiguous                      */
   void* o;                /* device; rows >= n_rows[b] are left as they were                */
   int64_t q_stride[3], o_stride[3]; /* sequence, row, head                                  */
-  const int32_t* ctx_len; /* host [batch], >= 0; ctx_len[b] + n_rows[b] <= max_ctx          */
+  const int32_t* ctx_len; /* host [batch], >= 0; ctx_len[b] + n_rows[b] <= max_ctx and 2^30 */
   const int32_t* n_rows;  /* host [batch], 0 .. max_rows; 0: the sequence has nothing to do */
   const uint32_t* mask;   /* device [batch][max_rows][(max_rows + 31) / 32]: bit j % 32 of word j / 32; null: all rows
                              of a sequence see one another (a block)                        */

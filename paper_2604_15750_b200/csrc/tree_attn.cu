@@ -118,10 +118,10 @@ TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, T
   for (int b = 0; b < in->batch; ++b) work += (long long)units[b] * tiles[b];
   auto rounds = [&](long long n, int slots, int t, int more) {
     const int one_each = slots / k.resident;
-    const long long left = n % slots, mean = n <= slots ? t * k.tile : work * k.tile / n;
+    const long long left = n % slots, mean = n <= slots ? (long long)t * k.tile : work * k.tile / n;
     const long long two = mean + k.rest + more, one = mean * k.tile_alone / k.tile + k.rest_alone + more;
     const long long last = left == 0 ? 0 : left <= one_each ? one : one + (two - one) * (left - one_each) / (slots - one_each);
-    const long long cost = n / slots * two + last, most = t * k.tile_alone + k.rest_alone + more;
+    const long long cost = n / slots * two + last, most = (long long)t * k.tile_alone + k.rest_alone + more;
     return cost > most ? cost : most;
   };
   // (an 8-bit cache's probabilities end 2^-27 below the largest of a stretch: tc_tree.cuh)
@@ -201,6 +201,8 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   if (in->max_rows < 1 || in->max_rows > DC_MAX_WINDOW) return op_fail(DC_ERR_SHAPE, "max_rows=%d outside [1, %d]", in->max_rows, (int)DC_MAX_WINDOW);
   if (!(in->scale >= 0.f) || in->scale > 1e30f) return op_fail(DC_ERR_INVALID_ARG, "scale outside [0, 1e30]");
   if ((rc = op_check_keys(c, in->batch, in->ctx_len, in->n_rows, in->max_rows, ", max_rows bounds the rows")) != DC_OK) return rc;
+  for (int b = 0; b < in->batch; ++b)
+    if (in->ctx_len[b] + in->n_rows[b] > kTreeMostKeys) return op_fail(DC_ERR_UNSUPPORTED, "sequence %d: more than %d keys", b, kTreeMostKeys);
   if ((long long)in->max_rows * in->n_q_heads > 524288) return op_fail(DC_ERR_UNSUPPORTED, "more than 524288 rows x query heads");
   return DC_OK;
 }

@@ -12,6 +12,7 @@
 namespace dc {
 
 constexpr int kTreeTile = 128;   // keys: stretches are whole tiles
+constexpr int kTreeMostKeys = 1 << 30;   // of a sequence: places of keys, and of the tiles behind the last one, are 32-bit numbers
 constexpr int kTreeMostTiles = 1024;     // of a stretch over an 8-bit cache on the tensor cores (tc_tree.cuh)
 
 struct TreeArgs {

@@ -24,3 +24,13 @@ def test_no_stretch_over_an_8_bit_cache_is_longer_than_2_to_the_17_keys():
     batch, hkv, keys = 8, 37, 1_310_720
     rc, need = workspace(keys - 1, 1, hkv, keys, batch, hkv)
     assert rc == 0 and need >= keys // 2 ** 17 * batch * hkv * (8 + 4 * 128)
+
+
+def test_contexts_of_more_than_2_to_the_30_keys_are_refused():
+    """Places of keys are 32-bit numbers, and those of the tiles behind the last one have to fit too."""
+    most = 2 ** 31 - 64
+    for hd, held, dtype in ((8, b.DC_E4M3, b.DC_BF16), (128, b.DC_E4M3, b.DC_BF16), (64, b.DC_F32, b.DC_F32)):
+        for ctx in (most - 1, 2 ** 30):
+            assert workspace(ctx, 1, 1, most, hd=hd, held=held, dtype=dtype)[0] == 3 and L.dc_last_error(None)
+        rc, need = workspace(2 ** 30 - 1, 1, 1, most, hd=hd, held=held, dtype=dtype)
+        assert rc == 0 and need > 0
