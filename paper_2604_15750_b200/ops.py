@@ -67,7 +67,8 @@ def _on_cuda(index):
         raise RuntimeError("the operators need tensors on a CUDA device; there is no CPU path")
 
 
-_current, _stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# (a torch without CUDA has neither)
+_current, _stream_of = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def _call(f, index, stream, *args):
