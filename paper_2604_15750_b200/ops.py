@@ -308,7 +308,11 @@ def tree_mask(parents, rows=None):
     for b, p in enumerate(parents):
         if len(p) > rows:
             raise ValueError(f"sequence {b} has {len(p)} rows, more than {rows}")
-        rc = _b.lib().dc_tree_mask((C.c_int32 * max(len(p), 1))(*[int(x) for x in p]), len(p), words, mask[b].data_ptr())
+        try:
+            parent = array("i", [int(x) for x in p] or [-1])
+        except OverflowError:
+            raise ValueError(f"sequence {b}: a parent is outside 32 bits") from None
+        rc = _b.lib().dc_tree_mask(C.cast(parent.buffer_info()[0], _b._I32P), len(p), words, mask[b].data_ptr())
         if rc != _b.DC_OK:
             raise _b.DepCapError(rc, _b.lib().dc_last_error(None).decode())
     return mask

@@ -216,3 +216,10 @@ def test_a_scale_that_fp32_does_not_hold_is_refused(scale):
     q = torch.zeros((2, 3, 4, 128), dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="scale"):
         dc.tree_attention(q, dc.KvCache(*_kv()), [0, 0], [3, 3], scale=scale)
+
+
+@pytest.mark.parametrize("p", [[2 ** 32 - 1, 0], [-1, 2 ** 32], [-1, -2 ** 32], [-1, 2 ** 70]])
+def test_parents_outside_32_bits_are_no_rows(p):
+    """Cut to 32 bits they would be -1 and 0."""
+    with pytest.raises((ValueError, dc.DepCapError)):
+        dc.tree_mask([p])
