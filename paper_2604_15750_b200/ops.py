@@ -75,7 +75,12 @@ def _call(f, index, stream, *args):
     """f(*args, stream) with device `index` current (-1: not a CUDA device)"""
     if index < 0:
         _on_cuda(index)
-    raw = _stream_of(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        raw = _stream_of(index)
+    else:
+        if stream.device_index != index:
+            raise ValueError(f"a stream of device {stream.device_index} for tensors of device {index}")
+        raw = stream.cuda_stream
     if index == _current():
         rc = f(*args, raw)
     else:
