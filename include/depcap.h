@@ -536,7 +536,8 @@ typedef struct dc_tree_in {
   int32_t max_rows;       /* 1 .. DC_MAX_WINDOW: row pitch of the mask                      */
   float scale;            /* 0: 1 / sqrt(head_dim); at most 1e30                            */
   const void* q;          /* device; the dims of a head are contiguous                      */
-  void* o;                /* device; rows >= n_rows[b] are left as they were                */
+  void* o;                /* device; rows >= n_rows[b] are left as they were; q itself (same pointer, same strides),
+                             or else without overlap with it and the cache                  */
   int64_t q_stride[3], o_stride[3]; /* sequence, row, head                                  */
   const int32_t* ctx_len; /* host [batch], >= 0; ctx_len[b] + n_rows[b] <= max_ctx and 2^30 */
   const int32_t* n_rows;  /* host [batch], 0 .. max_rows; 0: the sequence has nothing to do */

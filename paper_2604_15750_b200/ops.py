@@ -230,7 +230,7 @@ def qk_norm_rope(q, k, pos, q_gain=None, k_gain=None, eps=1e-5, rope_theta=10000
 def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, out=None, workspace=None, status=None, stream=None):
     """dc_tree_attention: q [sequences, rows, q heads, head_dim] over slot b's first ctx_len[b] keys and, by the mask, the
     n_rows[b] drafted ones behind them.  mask int32 [sequences, rows, (rows + 31) // 32] on the device (`tree_mask`); None: all
-    rows of a sequence see one another.  Returns out, like q; its rows >= n_rows[b] are left as they were (zeros in a new one).
+    rows of a sequence see one another.  Returns out, like q, or q itself; its rows >= n_rows[b] are left as they were (zeros in a new one).
     workspace: a uint8 tensor on the device for callers that keep one (`tree_attention_workspace` bytes)."""
     shape, dtype, index = q.shape, q.dtype, cache._index
     if len(shape) != 4 or shape[3] != cache.head_dim:
@@ -247,6 +247,8 @@ def tree_attention(q, cache, ctx_len, n_rows, mask=None, layer=0, scale=None, ou
         raise ValueError("the dims of a head are contiguous")
     if 0 in os_:
         _apart(shape, os_, "out")
+    if os_ != (a, b, h, d) and out.data_ptr() == q.data_ptr() and any(m > 1 and x != y for m, x, y in zip(shape, os_, (a, b, h, d))):
+        raise ValueError("an output in the place of its input has the same strides")
     mask_at = 0
     if mask is not None:
         if mask.dtype not in (torch.int32, torch.uint32) or mask.shape != (batch, rows, (rows + 31) // 32) or not mask.is_contiguous():

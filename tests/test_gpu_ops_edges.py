@@ -28,3 +28,23 @@ def test_calls_of_nothing(held):
         with pytest.raises(ValueError):
             dc.tree_attention(q, c, [9] * batch, [0] * (batch + 1))
     assert not c.k.view(torch.uint8).any() and not c.v.view(torch.uint8).any()
+
+
+@pytest.mark.parametrize("dtype,held,hd", [(BF16, E4M3, 128), (BF16, BF16, 128), (F32, F32, 64), (BF16, BF16, 96)])
+@pytest.mark.parametrize("ctx,rows,group", [([500] * 4, [9] * 4, 1), ([1000, 20], [100, 3], 2), ([40000, 20], [9, 3], 2)])
+def test_attention_in_the_place_of_the_queries(dtype, held, hd, ctx, rows, group):
+    """out = q: units on their own, joined by a cluster and by a launch give what they give elsewhere."""
+    g = torch.Generator().manual_seed(5)
+    B, H, most = len(ctx), 2, max(rows) + 2
+    if hd == 96:
+        ctx = [min(x, 5000) for x in ctx]
+    c = dc.KvCache.empty(1, B, H, (max(ctx) + most + 63) // 64 * 64, hd, held, DEV)
+    x = torch.randn((B, c.max_ctx, H, hd), generator=g).to(dtype).to(DEV)
+    dc.cache_write(c, x, x, [0] * B)
+    q = torch.randn((B, most, H * group, hd), generator=g).to(dtype).to(DEV)
+    mask = dc.tree_mask([[-1] + list(range(r - 1)) for r in rows], most).to(DEV)
+    want = dc.tree_attention(q, c, ctx, rows, mask)
+    got = q.clone()
+    assert dc.tree_attention(got, c, ctx, rows, mask, out=got) is got
+    for b, r in enumerate(rows):
+        assert torch.equal(got[b, :r], want[b, :r]) and torch.equal(got[b, r:], q[b, r:])

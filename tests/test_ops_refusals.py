@@ -223,3 +223,13 @@ def test_parents_outside_32_bits_are_no_rows(p):
     """Cut to 32 bits they would be -1 and 0."""
     with pytest.raises((ValueError, dc.DepCapError)):
         dc.tree_mask([p])
+
+
+def test_an_output_in_the_place_of_the_queries_has_their_strides():
+    """As of qk_norm_rope: at other strides a row's output lies where another row's queries still are."""
+    q = torch.zeros((2, 3, 4, 128), dtype=torch.bfloat16)
+    c = dc.KvCache(*_kv())
+    with pytest.raises(RuntimeError, match="no CPU path"):
+        dc.tree_attention(q, c, [0, 0], [3, 3], out=q)
+    with pytest.raises(ValueError, match="strides"):
+        dc.tree_attention(q, c, [0, 0], [3, 3], out=q.view(2, 4, 3, 128).transpose(1, 2))
