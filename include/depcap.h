@@ -532,7 +532,8 @@ typedef struct dc_tree_in {
   int32_t batch;          /* 1 .. min(max_batch, DC_MAX_BATCH)                              */
   int32_t layer;          /* of the cache                                                   */
   int32_t dtype;          /* of q and o, DC_F32 | DC_BF16; a cache that is not DC_E4M3 has the same */
-  int32_t n_q_heads;      /* a multiple of the cache's n_kv_heads                           */
+  int32_t n_q_heads;      /* a multiple of the cache's n_kv_heads, at most 2048 times as many; max_rows x n_q_heads at most
+                             524288; batch x rows x query heads of a kv head at most 65535 x 16, or x 32 on the tensor cores */
   int32_t max_rows;       /* 1 .. DC_MAX_WINDOW: row pitch of the mask                      */
   float scale;            /* 0: 1 / sqrt(head_dim); at most 1e30                            */
   const void* q;          /* device; the dims of a head are contiguous                      */

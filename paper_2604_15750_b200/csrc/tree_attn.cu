@@ -207,6 +207,10 @@ int check(const dc_cache* c, const dc_tree_in* in) {
   return DC_OK;
 }
 
+int check_grid(const dc_cache* c, const dc_tree_in* in, const TreePlan& p) {
+  return c->n_kv_heads <= 65535 && (long long)p.line_tiles * in->batch <= 65535 ? DC_OK : op_fail(DC_ERR_UNSUPPORTED, "more rows x query heads than one call takes");
+}
+
 template <typename T, typename H, int HD, int L>
 bool launch_simt_hd(const TreeArgs& a, const TreePlan& p, int batch, cudaStream_t s) {
   static std::atomic<unsigned long long> done;
@@ -268,19 +272,21 @@ extern "C" int dc_tree_attention_workspace(const dc_cache* cache, const dc_tree_
   const int rc = check(cache, in);
   if (rc != DC_OK) return rc;
   if (!bytes) return op_fail(DC_ERR_INVALID_ARG, "null argument");
-  *bytes = plan(cache, in).bytes;
-  return DC_OK;
+  const TreePlan p = plan(cache, in);
+  const int fits = check_grid(cache, in, p);
+  if (fits == DC_OK) *bytes = p.bytes;
+  return fits;
 }
 
 extern "C" int dc_tree_attention(const dc_cache* cache, const dc_tree_in* in, void* cuda_stream) {
-  const int rc = check(cache, in);
+  int rc = check(cache, in);
   if (rc != DC_OK) return rc;
   if (!in->q || !in->o) return op_fail(DC_ERR_INVALID_ARG, "null argument");
   const TreePlan p = plan(cache, in);
   if (p.lines == 0) return DC_OK;
+  if ((rc = check_grid(cache, in, p)) != DC_OK) return rc;
   if (p.bytes && (!in->workspace || !op_aligned(in->workspace) || in->workspace_bytes < p.bytes))
     return op_fail(DC_ERR_INVALID_ARG, "the workspace needs %llu bytes on a 16-byte boundary", (unsigned long long)p.bytes);
-  if (cache->n_kv_heads > 65535 || (long long)p.line_tiles * in->batch > 65535) return op_fail(DC_ERR_UNSUPPORTED, "too many heads");
   TreeArgs a;
   a.c = *cache;
   const size_t layer = (size_t)in->layer * cache->max_batch * cache->n_kv_heads * cache->max_ctx;   // keys

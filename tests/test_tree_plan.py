@@ -34,3 +34,9 @@ def test_contexts_of_more_than_2_to_the_30_keys_are_refused():
             assert workspace(ctx, 1, 1, most, hd=hd, held=held, dtype=dtype)[0] == 3 and L.dc_last_error(None)
         rc, need = workspace(2 ** 30 - 1, 1, 1, most, hd=hd, held=held, dtype=dtype)
         assert rc == 0 and need > 0
+
+
+def test_more_units_than_a_grid_has_are_refused_when_the_workspace_is_asked_for():
+    """Not by the call alone, when its workspace has been made."""
+    for rows, batch, hd, rc in ((256, 31, 256, 0), (256, 32, 256, 3)):
+        assert workspace(10, rows, 128, 512, batch=batch, hd=hd)[0] == rc
