@@ -80,9 +80,10 @@ struct TreePlan {
 
 // What units of one kernel take, in 10 ns, measured where K and V come from L2: a tile of 128 keys and the rest of a unit (barriers,
 // queries, the first loads' way, the output), with every place of the SMs taken and with one unit an SM; and what it takes more as a
-// CTA of a cluster
+// CTA of a cluster.  kCost64 and kCost128 are of fp32 caches; bf16 and e4m3 ones, which take the same kernel with a conversion on the
+// way, go by them too
 struct TreeCost { int lines, resident, tile, rest, tile_alone, rest_alone, cluster; };
-constexpr TreeCost kCost8[3] = {{32, 2, 111, 450, 85, 310, 100}, {64, 1, 97, 470, 97, 470, 350}, {128, 1, 146, 790, 146, 790, 500}};
+constexpr TreeCost kCost8[3] = {{32, 2, 125, 450, 92, 310, 100}, {64, 1, 101, 470, 101, 470, 350}, {128, 1, 160, 790, 160, 790, 500}};
 constexpr TreeCost kCost16[3] = {{32, 1, 67, 250, 67, 250, 100}, {64, 1, 74, 350, 74, 350, 350}, {128, 1, 128, 660, 128, 660, 500}};
 constexpr TreeCost kCost64[3] = {{8, 3, 870, 30, 760, 30, 0}, {32, 2, 980, 230, 950, 200, 0}, {64, 2, 1744, 610, 1680, 570, 0}};    // k_tree_simt_hd
 constexpr TreeCost kCost128[3] = {{8, 3, 1640, 50, 1430, 30, 0}, {32, 2, 1820, 420, 1750, 390, 0}, {64, 1, 2535, 770, 2535, 770, 0}};
@@ -91,8 +92,8 @@ constexpr TreeCost kCostAny = {kTreeLines, 2, 2000, 500, 2000, 500, 0};
 constexpr int kJoinLaunch = 300, kJoinLines8 = 8;
 
 // The stretch that ends first: units of about the mean length in rounds of as many as run at once, but not before the longest one
-// and not before the keys have come from memory.  (26 drawn calls, each with up to 21 forced widths and stretches: what this picks takes
-// 1.02 times the best in the mean, 1.15 at worst; 64 to 128 lines over e4m3 took up to 1.8 times as long without the clusters' places
+// and not before the keys have come from memory.  (20 drawn calls over e4m3, each with up to 21 forced widths and stretches: what this picks
+// takes 1.01 times the best in the mean, 1.12 at worst; 64 to 128 lines over e4m3 took up to 1.8 times as long without the clusters' places
 // and the cost of joining.)
 template <typename Slots>
 TreePlan make_plan(const dc_cache* c, const dc_tree_in* in, const TreeCost& k, TreePlan::Kind kind, Slots in_clusters) {
