@@ -293,9 +293,11 @@ extern "C" int dc_qk_norm_rope(const dc_qk_in* in, void* cuda_stream) {
   }
   a.heads[0] = in->n_q_heads; a.heads[1] = in->n_kv_heads;
   a.pos = in->pos; a.rows = in->rows; a.hd = in->head_dim; a.eps = in->eps;
-  const double step = pow((double)in->rope_theta, -2.0 / in->head_dim);
-  double f = 1.0;
-  for (int i = 0; i < 128; ++i) { a.freq[i] = f; f *= step; }   // (off by at most i roundings of 2^-53)
+  // (products of up to 127 factors: in the 64 bits of a long double they are off by 2^-57, in a double by 2^-46, which are 2e-6 of a
+  // radian at position 2^31)
+  const long double step = powl((long double)in->rope_theta, -2.0L / in->head_dim);
+  long double f = 1.0L;
+  for (int i = 0; i < 128; ++i) { a.freq[i] = i < in->head_dim / 2 ? (double)f : 0.0; f *= step; }
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (in->dtype == DC_F32 ? launch_vec<float>(a, s) : launch_vec<__nv_bfloat16>(a, s)) return op_launched("dc_qk_norm_rope");
   const int heads = a.heads[0] + a.heads[1];

@@ -48,3 +48,18 @@ def test_attention_in_the_place_of_the_queries(dtype, held, hd, ctx, rows, group
     assert dc.tree_attention(got, c, ctx, rows, mask, out=got) is got
     for b, r in enumerate(rows):
         assert torch.equal(got[b, :r], want[b, :r]) and torch.equal(got[b, r:], q[b, r:])
+
+
+@pytest.mark.parametrize("theta,hd", [(10.0, 256), (10.0, 128), (1e4, 256), (2.0, 96)])
+def test_the_farthest_positions_keep_their_angles(theta, hd):
+    """An angle of 2^31 x a frequency is 2^53 of its own roundings away from a turn only if the frequency is off by one of them:
+    the tolerance has none beside it."""
+    import ops_ref as ref
+    g = torch.Generator().manual_seed(7)
+    q, k = (torch.randn((500, 3, hd), generator=g) for _ in range(2))
+    pos = torch.randint(2 ** 30, 2 ** 31 - 1, (500,), generator=g, dtype=torch.int32)
+    outs = dc.qk_norm_rope(q.to(DEV), k.to(DEV), pos.to(DEV), eps=1e-6, rope_theta=theta)
+    for got, x in zip(outs, (q, k)):
+        want, size = ref.rope(x, pos, None, 1e-6, theta)
+        over = (got.cpu().double() - want).abs() / ref.rope_tolerance(want, size, F32)
+        assert (over <= 1).all(), float(over.max())
