@@ -485,7 +485,8 @@ typedef struct dc_cache_rows {
   int32_t dtype;          /* of the rows, DC_F32 | DC_BF16; a cache that is not DC_E4M3 has the same */
   void *k, *v;            /* device; starts of layer 0, sequence 0, row 0, kv head 0, dim 0 */
   int64_t k_stride[5];    /* layer, sequence, row, kv head, dim: any, but 16-byte rows that */
-  int64_t v_stride[5];    /* start on 16-byte boundaries move fastest (V: dims or keys as the contiguous axis) */
+  int64_t v_stride[5];    /* start on 16-byte boundaries move fastest (V: dims or keys as the contiguous axis;
+                             with keys pos[b] is a multiple of 16 bytes of them too, else it takes 13 times as long) */
   const int32_t* pos;     /* host [batch], >= 0                                             */
   const int32_t* n;       /* host [batch], >= 0 rows; pos[b] + n[b] <= max_ctx              */
 } dc_cache_rows;

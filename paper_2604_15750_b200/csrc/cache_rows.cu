@@ -13,7 +13,8 @@ struct RowsArgs {
 };
 
 // ---- any strides, types and alignment: a warp takes one row of K or V -----------------------------------
-// (32 layers of four contexts of up to 1024 keys 6353 us, 13 times k_rows_tile: V goes out value by value)
+// (32 layers of four contexts of up to 1024 keys 6353 us, 13 times k_rows_tile: V goes out value by value.  V with contiguous keys comes
+// here, K with it, where a first position is no multiple of 16 bytes: its pieces would lie across the cache's)
 // grid (row, sequence * kv head, layer * 2 + side)
 constexpr int kAnyWarps = 8;
 
@@ -71,8 +72,9 @@ __global__ void __launch_bounds__(kAnyWarps * 32) k_rows_any(const RowsArgs a) {
 //   K, either way: 16 (8) lanes a row, 8 dims a lane.
 //   V with contiguous dims: the same, four keys a thread, whose values turn into groups of four keys in shared memory.
 //   V with contiguous keys (ACROSS): 8 keys x 1 dim a lane; a row's maximum comes together over the CTA.
-// Bound by HBM (2 bytes read for 1 written): 32 layers of four contexts of up to 1024 keys, 2.87 GB, 481 us (6.0 TB/s) with contiguous keys,
-// 594 us with contiguous dims (5.5); 28 layers of four contexts of 768 keys back, 267 MB, 41 us (6.5).  Ordinary instructions for a value: one to unpack, one for the maximum (of 16-bit
+// Bound by HBM (2 bytes read for 1 written): 32 layers of four contexts of up to 1024 keys, 2.87 GB, 480 us (6.0 TB/s; 516 .. 534 where
+// passes go on for a second) with contiguous keys, 543 us with contiguous dims (5.3); 28 layers of four contexts of 768 keys back, 267
+// MB, 41 us (6.5), as rows 58 (4.6); 16 layers of a bf16 cache written 308 us (6.2), read as rows 378 (5.0).  Ordinary instructions for a value: one to unpack, one for the maximum (of 16-bit
 // patterns, two at a time), a half to multiply, a half to convert.
 constexpr int kTk = 64, kTileThreads = 256;
 

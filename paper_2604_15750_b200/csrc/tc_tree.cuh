@@ -27,15 +27,16 @@
 // P lies in shared memory as the threads have it, a row of N values for a key (the product takes it with the lines as the
 // contiguous axis): a thread stores 16 bytes at a time, where rows of keys would take a store for every value.
 //
-// Measured (device time): 16 x 4096 keys of 32 heads, 32 rows, e4m3, 566 MB: 99 us, 5.7 TB/s; 8 x 900..1200 keys, 24 rows, 77 MB: 20.4
-// us (3.8 TB/s; a unit's start and end are a third); 4 x 768 keys of 4 heads, 64 rows of 7 heads a group, bf16: 10.9 us (seven
-// tiles one after the other, 1250 clk each); one row over 512 keys of 32 heads: 8.0 us.
+// Measured (device time of 21 passes): 16 x 4096 keys of 32 heads, 32 rows, e4m3, 566 MB: 102 us, 5.5 TB/s (119 us where passes go on for
+// a second, 4.8); 8 x 900..1200 keys, 24 rows, 77 MB: 21.2 us (3.6 TB/s; a unit's start and end are a third); 4 x 768 keys of 4 heads,
+// 64 rows of 7 heads a group, bf16: 11.0 us (seven tiles one after the other, 1250 clk each); one row over 512 keys of 32 heads:
+// 8.3 us.  The third part of P costs 1 to 5% of these over e4m3.
 //
 // Why N = 32, 64 or 128: a column costs softmax time whether it has a line or not, and every further unit streams the keys again.
 // 32 lines and e4m3 leave room for two CTAs on an SM, whose starts and softmax overlap.  128 lines take in 64 KB of bf16 a tile for
-// four times as many as 32: 4 x 4000 keys, 128 rows of 7 heads 52 us, with 64 lines 67.  Over e4m3 the
-// softmax bounds: a tile of 64 lines takes 0.73 us of 128, 0.97 alone, 1.1 as two of 32 (12 x 4635 keys of 8 heads, 121 rows of 4 heads a
-// group 190 us, 128 with half the heads).  Which one is taken: kCost8, kCost16 (tree_attn.cu).
+// four times as many as 32: 4 x 4000 keys, 128 rows of 7 heads 49 us, with 64 lines 67.  Over e4m3 the
+// softmax bounds: a tile of 64 lines takes 0.80 us of 128, 1.01 alone, 1.25 as two of 32 (12 x 4635 keys of 8 heads, 121 rows of 4 heads a
+// group 225 us).  Which one is taken: kCost8, kCost16 (tree_attn.cu).
 //
 // Warps: 0 = TMA producer (K and V^T rings), 1 = TMEM owner and issuer of S^T, 2 = issuer of O^T, which first puts V^T tiles in order
 // (clears keys beyond the last; a drafted key's values that are not finite are cleared and noted, because 0 times them
@@ -52,13 +53,13 @@ struct TreeTc {
   static constexpr int kLines = N == 128 ? 32 : 16;             // lines of a softmax warp, in chunks of 16
   static constexpr int kGroups = N / kLines, kThreads = 128 + 128 * kGroups;
   static constexpr int kSlot = Q8 ? kSub : 2 * kSub;           // a tile of K or of V^T
-  // slots of the rings, as shared memory has room
+  // slots of the rings, as shared memory has room (128 lines over e4m3: 2 + 3 or 3 + 2, the same to 0.5%)
   static constexpr int kRingK = N == 32 ? (Q8 ? 2 : 3) : N == 64 ? (Q8 ? 4 : 3) : 2;
   static constexpr int kP = Q8 && N >= 64 ? 2 : 1;             // tiles of P: with two no warp waits for the product before
   static constexpr int kRingV = N == 32 || (Q8 && N == 128) ? 3 : kRingK;
   // Half of the softmax warps turn scores into P while the other half reads and scales its scores: left alone all warps do the
-  // same at the same time, and the unit for 2^x is idle for the rest (a tile of 128 x 128 1.80 -> 1.46 us, 64 lines 1.07 -> 0.97; with
-  // 128 lines over bf16 1.25 -> 1.68)
+  // same at the same time, and the unit for 2^x is idle for the rest (with two parts of P a tile of 128 x 128 1.80 -> 1.46 us, 64
+  // lines 1.07 -> 0.97; with 128 lines over bf16 1.25 -> 1.68)
   static constexpr bool kTurns = Q8 && N >= 64;
   static constexpr int kResident = Q8 && N == 32 ? 2 : 1;      // CTAs of an SM
   static constexpr int kOperand = N * 256;                     // bytes of Q

@@ -96,8 +96,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_tree_join(const __grid_cons
 // and V are on their way (fp32: straight to shared memory) while these are worked on; 128, where two tiles have no room: the next K
 // while V is worked on, and V while K is.  Drafted keys behind the last one that a line of the unit sees are left out.
 // fp32, 64 rows of 4 heads a group, 4 x 2064 keys of 4 heads: head_dim 64 105 us, 128 183 us (2 lines x 4 keys a thread and single
-// multiply-adds 137 and 264): 45% of the multiply-adds' full rate, because two to three CTAs of four warps do not hide the latency of
-// shared memory, and more have no room.  9 rows, 14 x 2260 keys: 87 us (133).
+// multiply-adds 137 and 264): 20.6 TFLOP/s, 28% of the multiply-adds' full rate, because two to three CTAs of four warps do not hide the
+// latency of shared memory, and more have no room; bf16 the same (109 us), fp32 rows over e4m3, 128 dims 196 us (with 64 lines it spills).  9 rows, 14 x 2260 keys: 87 us (133).
 constexpr int kSimtKeys = 64, kSimtThreads = 128;
 __host__ __device__ constexpr int tree_simt_smem_hd(int hd, int l) {
   return (8 * l * (hd + 4) + (hd == 64 ? 2 : 1) * (kSimtKeys * (hd + 4) + hd * (kSimtKeys + 4)) + 8 * l * (kSimtKeys + 4)) * 4;
